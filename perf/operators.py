@@ -292,7 +292,7 @@ def _tables(s):
     b = torch.searchsorted(cu, t, right=True) - 1
     pos = held[b] + t - cu[b]
     slots = torch.where(ok[b], table[b, (pos // PT).clamp(max=table.shape[1] - 1)].long() * PT + pos % PT, -1)
-    taken = torch.where(ok, upto, 0).amax()
+    taken = torch.where(ok & (need > 0), upto, 0).amax()
     return {"table": table, "cu": cu.to(torch.int32), "lens": torch.where(ok, held + add, -1).to(torch.int32), "slots": slots, "first": (s["first"] + taken).to(torch.int32)}
 
 
