@@ -54,7 +54,7 @@ extern "C" {
 
 typedef struct fastar_cache fastar_cache_t;          /* opaque host object */
 
-typedef enum { FASTAR_BF16 = 0, FASTAR_FP32 = 1 } fastar_dtype_t;
+typedef enum { FASTAR_BF16 = 0, FASTAR_FP32 = 1, FASTAR_FP16 = 2 /* dense path only */ } fastar_dtype_t;
 
 typedef struct {
   int32_t num_heads;         /* H >= 1 */
@@ -367,6 +367,78 @@ int fastar_annca_select_noalloc(const void* q, const void* k_prompt, int32_t num
  * returns FASTAR_OK or the first error a kernel of fastar_annca_select_noalloc recorded on the current
  * device since the last read, and clears it.  Allocates nothing; not for use during stream capture. */
 int fastar_noalloc_last_status(void* stream);
+
+/* ---- The dense path of several rollouts ------------------------------------------------------------------------
+ * The method runs dense for the first denoising steps and in part of the layers (Section 6, implementation details;
+ * Eq. 1).  These calls serve such layers for several rollouts (sequences) at once: causal attention over the packed
+ * prompts or first chunks, a paged cache of 8-bit codes that holds every token, attention over that cache with one
+ * token or a chunk per sequence, and the page tables for it.
+ *
+ * Packed tensors: the tokens of all sequences lie one after the other on the token axis of [head][T][d]; sequence b has
+ * the tokens [cu[b], cu[b+1]), cu: dev int32 [num_seqs + 1], and n_b of them.  Tokens that no sequence has are neither
+ * read nor written.  lens: dev int32 [num_seqs], the sequence's keys after its new tokens are in the cache: new token i
+ * has position lens[b] - n_b + i.  lens[b] < 0 (what fastar_block_tables writes for a refused request): the
+ * sequence is passed over, its rows are left as they were.
+ * The cache: k_codes, v_codes: dev uint8 [num_pages][num_kv_heads][page_tokens][d], fp8 e4m3 codes; k_scale, v_scale: dev fp32
+ * [num_pages][num_kv_heads]; an element is code x scale.  table: dev int32 [num_seqs][table_width], page of tokens
+ * [i page_tokens, (i+1) page_tokens) of the sequence.  All contiguous.  page_tokens: 64 or 128; d: 64 or 128.
+ * dtype: FASTAR_BF16 or FASTAR_FP16, of q, k, v and out; fp32 accumulation and soft-max.  num_heads is a multiple of num_kv_heads;
+ * query head h reads key head h / (num_heads / num_kv_heads).  Strides as elsewhere; rows do not overlap.
+ * Frames: a token sees the keys of its sequence up to the end of its own frame of frame_len tokens (positions
+ * [0, (floor(position / frame_len) + 1) frame_len)), frame_len = 1 being the causal mask; 0: all keys of the sequence.
+ * What is not seen has no influence, whatever its bits are.  A row that sees only logits of -inf gives zeros.
+ * max_new, max_len: what no n_b and no lens[b] exceeds (they size the launch; 1 <= max_new, max_new <= max_len).
+ * The device used is the current one.  Lengths, tables and page numbers that the host cannot see are checked on the
+ * device: a sequence whose entries are out of range (cu not ascending within [0, T], n_b > max_new, lens[b] > max_len, lens[b] <
+ * n_b) is passed over, a page outside the pool is not written and page 0 is read in its place; the first such finding stays in
+ * a status word of the library (FASTAR_ERR_BOUNDS) until fastar_dense_last_status reads it.  The first of these calls on a
+ * device looks that word up; make it before any stream capture starts.  Later calls may be captured. */
+
+/* Page tables and slots from the requests' lengths.  Request b holds held[b] tokens in the first ceil(held[b] / page_tokens) pages
+ * of its row and adds add[b]; the pages that this takes come off the free list free_pages[first .. num_free), in the order of the
+ * requests.  A request is refused as a whole if its row is too short or if the list does not reach for what it and all those before
+ * it need (requests whose row is too short need nothing); one that needs no page is never refused for the list.  Outputs: table (new
+ * entries of accepted requests written, all others left), cu [num_seqs + 1] (prefix sums of add, refused requests included), lens
+ * [num_seqs] (held + add, or -1), slots [max_add] int64 (page * page_tokens + row of every new token; -1 for refused ones and from the
+ * last token on), first_out [1] (first + pages taken).  held, add, first: dev int32; first_out and lens are not in place.  Tokens beyond
+ * max_add are cut off and their requests refused, negative lengths refuse the request (FASTAR_ERR_BOUNDS in the status word); a list
+ * that is too short leaves FASTAR_ERR_CAPACITY there. */
+int fastar_block_tables(const int32_t* held, const int32_t* add, int32_t num_seqs, int32_t page_tokens, const int32_t* free_pages,
+                        int32_t num_free, const int32_t* first, int32_t* table, int32_t table_width, int32_t* cu, int32_t* lens,
+                        int64_t* slots, int32_t max_add, int32_t* first_out, void* stream);
+
+/* New rows into the cache: k_new, v_new dev [num_kv_heads][T][d].  The scale of a page and head is the least power of two s with |x| / s <= 448
+ * for all its rows (2^-126 at least); codes are x / s rounded to the nearest even.  A page whose first row is written by this call starts anew;
+ * in one that has rows already the scale only grows, and they are recoded (exactly, but for codes below e4m3's least normal number).  Values that
+ * are not finite do not count towards the scale and become the code that is no number.  Other rows are left as they were.  A page that is written
+ * belongs to one sequence of the call. */
+int fastar_kv8_append(const void* k_new, const void* v_new, int64_t head_stride, int64_t token_stride, uint8_t* k_codes, uint8_t* v_codes,
+                      float* k_scale, float* v_scale, int32_t num_pages, int32_t page_tokens, const int32_t* table, int32_t table_width,
+                      const int32_t* lens, const int32_t* cu, int32_t num_seqs, int32_t total_tokens, int32_t num_kv_heads, int32_t head_dim,
+                      int32_t dtype, void* stream);
+
+/* Attention of the new tokens (q, out: dev [num_heads][T][d], same strides) over the cache, their own keys included (append first).
+ * One token a sequence, a few, or thousands; sequences of all lengths in one call.  workspace: dev, 16-byte aligned, of at least
+ * fastar_kv8_attention_workspace_bytes (0 on invalid arguments; else 16 or more), contents irrelevant before and after; it
+ * belongs to one call at a time. */
+size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
+                                            int32_t num_kv_heads, int32_t head_dim);
+int fastar_kv8_attention(const void* q, void* out, int64_t head_stride, int64_t token_stride, const uint8_t* k_codes, const uint8_t* v_codes,
+                         const float* k_scale, const float* v_scale, int32_t num_pages, int32_t page_tokens, const int32_t* table,
+                         int32_t table_width, const int32_t* lens, const int32_t* cu, int32_t num_seqs, int32_t total_tokens, int32_t max_new,
+                         int32_t max_len, int32_t num_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype, int32_t frame_len,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of packed sequences over their own tokens: q, out dev [num_heads][T][d] (same strides), k, v dev [num_kv_heads][T][d] (same
+ * strides); max_tokens: what no sequence exceeds. */
+int fastar_packed_attention(const void* q, const void* k, const void* v, void* out, int64_t head_stride, int64_t token_stride,
+                            int64_t kv_head_stride, int64_t kv_token_stride, const int32_t* cu, int32_t num_seqs, int32_t total_tokens,
+                            int32_t max_tokens, int32_t num_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype, int32_t frame_len,
+                            void* stream);
+
+/* Synchronises `stream`, returns FASTAR_OK or the first error a kernel of the dense path recorded on the current device since the last read,
+ * and clears it.  Not for use during stream capture. */
+int fastar_dense_last_status(void* stream);
 
 /* Measurement aid (no counterpart in the paper).  While enabled, every hot kernel launch is bracketed
  * by a pair of CUDA events recorded on the launching stream.  fastar_profile_read synchronises the

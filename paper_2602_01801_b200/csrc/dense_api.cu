@@ -1,0 +1,160 @@
+// C entries of the dense path (include/fastar.h): argument checks and the choice of kernels.  No device memory is allocated here.
+#include <cudaTypedefs.h>
+
+#include <mutex>
+
+#include "common.h"
+#include "dense.h"
+
+namespace fastar {
+
+// First error of the dense path's kernels on a device; zero when the library is loaded.
+static __device__ int32_t g_dense_status;
+
+namespace {
+std::mutex g_dense_mu;
+int32_t* g_dense_word[64] = {};
+
+int dense_device(int32_t** status) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FASTAR_ERR_CUDA;
+  if (dev < 0 || dev >= 64) return FASTAR_ERR_INVALID_ARG;
+  std::lock_guard<std::mutex> lock(g_dense_mu);
+  if (!g_dense_word[dev]) {
+    int major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return FASTAR_ERR_CUDA;
+    if (major != 10) return FASTAR_ERR_NOT_SM100;
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_dense_status) != cudaSuccess || !p) return FASTAR_ERR_CUDA;
+    g_dense_word[dev] = static_cast<int32_t*>(p);
+  }
+  *status = g_dense_word[dev];
+  return FASTAR_OK;
+}
+
+bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+// Rows of `heads` heads: 16-byte pieces, not overlapping
+bool rows_ok(const void* p, int64_t hs, int64_t ts, int heads, int d) {
+  return p && aligned(p, 16) && hs >= 0 && ts >= d && hs % 8 == 0 && ts % 8 == 0 && (heads == 1 || hs >= d);
+}
+int shape_ok(int H, int KV, int D, int dtype) {
+  if (KV < 1 || H < KV || H % KV != 0) return FASTAR_ERR_INVALID_ARG;
+  if (dtype != FASTAR_BF16 && dtype != FASTAR_FP16) return FASTAR_ERR_INVALID_ARG;
+  if (D != 64 && D != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (H > 65535) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  return FASTAR_OK;
+}
+}  // namespace
+}  // namespace fastar
+
+using namespace fastar;
+
+extern "C" int fastar_block_tables(const int32_t* held, const int32_t* add, int32_t num_seqs, int32_t page_tokens, const int32_t* free_pages,
+                                   int32_t num_free, const int32_t* first, int32_t* table, int32_t table_width, int32_t* cu, int32_t* lens,
+                                   int64_t* slots, int32_t max_add, int32_t* first_out, void* stream) {
+  if (!held || !add || !free_pages || !first || !table || !cu || !lens || !first_out || (!slots && max_add > 0)) return FASTAR_ERR_INVALID_ARG;
+  if (num_seqs < 1 || num_free < 0 || table_width < 1 || max_add < 0 || first == first_out || held == lens || add == lens) return FASTAR_ERR_INVALID_ARG;
+  if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (!aligned(held, 4) || !aligned(add, 4) || !aligned(free_pages, 4) || !aligned(first, 4) || !aligned(table, 4) || !aligned(cu, 4) || !aligned(lens, 4) ||
+      !aligned(slots, 8) || !aligned(first_out, 4))
+    return FASTAR_ERR_INVALID_ARG;
+  int32_t* status = nullptr;
+  const int r = dense_device(&status);
+  if (r != FASTAR_OK) return r;
+  return launch_block_tables(held, add, num_seqs, page_tokens, free_pages, num_free, first, table, table_width, cu, lens, slots, max_add, first_out, status,
+                             static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int fastar_kv8_append(const void* k_new, const void* v_new, int64_t head_stride, int64_t token_stride, uint8_t* k_codes, uint8_t* v_codes,
+                                 float* k_scale, float* v_scale, int32_t num_pages, int32_t page_tokens, const int32_t* table, int32_t table_width,
+                                 const int32_t* lens, const int32_t* cu, int32_t num_seqs, int32_t total_tokens, int32_t num_kv_heads, int32_t head_dim,
+                                 int32_t dtype, void* stream) {
+  int r = shape_ok(num_kv_heads, num_kv_heads, head_dim, dtype);
+  if (r != FASTAR_OK) return r;
+  if (num_seqs < 1 || total_tokens < 0 || num_pages < 1 || table_width < 1 || !table || !lens || !cu) return FASTAR_ERR_INVALID_ARG;
+  if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (!k_codes || !v_codes || !k_scale || !v_scale || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
+    return FASTAR_ERR_INVALID_ARG;
+  if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
+  if (total_tokens == 0) return FASTAR_OK;
+  if (!rows_ok(k_new, head_stride, token_stride, num_kv_heads, head_dim) || !rows_ok(v_new, head_stride, token_stride, num_kv_heads, head_dim))
+    return FASTAR_ERR_INVALID_ARG;
+  AppendArgs a{};
+  a.k = k_new; a.v = v_new; a.hs = head_stride; a.ts = token_stride;
+  a.T = total_tokens; a.B = num_seqs; a.KV = num_kv_heads; a.D = head_dim; a.PT = page_tokens; a.W = table_width; a.pages = num_pages;
+  a.kc = k_codes; a.vc = v_codes; a.ks = k_scale; a.vs = v_scale;
+  a.table = table; a.lens = lens; a.cu = cu;
+  r = dense_device(&a.status);
+  if (r != FASTAR_OK) return r;
+  return launch_kv8_append(a, dtype == FASTAR_FP16, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
+                                                       int32_t num_kv_heads, int32_t head_dim) {
+  if (shape_ok(num_heads, num_kv_heads, head_dim, FASTAR_BF16) != FASTAR_OK || num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new) return 0;
+  return 16;
+}
+
+extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_stride, int64_t token_stride, const uint8_t* k_codes, const uint8_t* v_codes,
+                                    const float* k_scale, const float* v_scale, int32_t num_pages, int32_t page_tokens, const int32_t* table,
+                                    int32_t table_width, const int32_t* lens, const int32_t* cu, int32_t num_seqs, int32_t total_tokens, int32_t max_new,
+                                    int32_t max_len, int32_t num_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype, int32_t frame_len,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  int r = shape_ok(num_heads, num_kv_heads, head_dim, dtype);
+  if (r != FASTAR_OK) return r;
+  if (num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new || frame_len < 0 || num_pages < 1 || table_width < 1) return FASTAR_ERR_INVALID_ARG;
+  if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (max_len > static_cast<int64_t>(table_width) * page_tokens) return FASTAR_ERR_INVALID_ARG;
+  if (!table || !lens || !cu || !aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
+  if (!k_codes || !v_codes || !k_scale || !v_scale || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
+    return FASTAR_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 16) ||
+      workspace_bytes < fastar_kv8_attention_workspace_bytes(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim))
+    return FASTAR_ERR_WORKSPACE;
+  if (total_tokens == 0) return FASTAR_OK;
+  if (!rows_ok(q, head_stride, token_stride, num_heads, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, head_dim)) return FASTAR_ERR_INVALID_ARG;
+  DenseArgs a{};
+  a.q = q; a.out = out; a.q_hs = head_stride; a.q_ts = token_stride;
+  a.T = total_tokens; a.B = num_seqs; a.H = num_heads; a.KV = num_kv_heads; a.G = num_heads / num_kv_heads;
+  a.cu = cu; a.frame = frame_len; a.max_new = max_new; a.max_len = max_len;
+  a.kc = k_codes; a.vc = v_codes; a.ks = k_scale; a.vs = v_scale; a.table = table; a.lens = lens;
+  a.W = table_width; a.pages = num_pages; a.PT = page_tokens;
+  a.parts = 1; a.chunk = max_len;
+  r = dense_device(&a.status);
+  if (r != FASTAR_OK) return r;
+  return launch_dense_rows(a, head_dim, dtype == FASTAR_FP16, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int fastar_packed_attention(const void* q, const void* k, const void* v, void* out, int64_t head_stride, int64_t token_stride,
+                                       int64_t kv_head_stride, int64_t kv_token_stride, const int32_t* cu, int32_t num_seqs, int32_t total_tokens,
+                                       int32_t max_tokens, int32_t num_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype, int32_t frame_len,
+                                       void* stream) {
+  int r = shape_ok(num_heads, num_kv_heads, head_dim, dtype);
+  if (r != FASTAR_OK) return r;
+  if (num_seqs < 1 || total_tokens < 0 || max_tokens < 1 || frame_len < 0 || !cu || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
+  if (total_tokens == 0) return FASTAR_OK;
+  if (!rows_ok(q, head_stride, token_stride, num_heads, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, head_dim)) return FASTAR_ERR_INVALID_ARG;
+  if (!rows_ok(k, kv_head_stride, kv_token_stride, num_kv_heads, head_dim) || !rows_ok(v, kv_head_stride, kv_token_stride, num_kv_heads, head_dim))
+    return FASTAR_ERR_INVALID_ARG;
+  DenseArgs a{};
+  a.q = q; a.out = out; a.q_hs = head_stride; a.q_ts = token_stride;
+  a.T = total_tokens; a.B = num_seqs; a.H = num_heads; a.KV = num_kv_heads; a.G = num_heads / num_kv_heads;
+  a.cu = cu; a.frame = frame_len; a.max_new = max_tokens; a.max_len = max_tokens;
+  a.k = k; a.v = v; a.kv_hs = kv_head_stride; a.kv_ts = kv_token_stride;
+  a.parts = 1; a.chunk = max_tokens;
+  r = dense_device(&a.status);
+  if (r != FASTAR_OK) return r;
+  return launch_dense_rows(a, head_dim, dtype == FASTAR_FP16, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int fastar_dense_last_status(void* stream) {
+  int32_t* word = nullptr;
+  const int r = dense_device(&word);
+  if (r != FASTAR_OK) return r;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t status = 0;
+  if (cudaMemcpyAsync(&status, word, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess) return FASTAR_ERR_CUDA;
+  if (cudaMemsetAsync(word, 0, 4, st) != cudaSuccess) return FASTAR_ERR_CUDA;
+  if (cudaStreamSynchronize(st) != cudaSuccess) return FASTAR_ERR_CUDA;
+  return status;
+}

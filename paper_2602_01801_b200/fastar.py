@@ -14,7 +14,7 @@ _lib = None
 
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED_SHAPE, ERR_CAPACITY, ERR_CUDA, ERR_TIMEOUT, ERR_NOT_SM100, ERR_WORKSPACE, ERR_BOUNDS = range(-1, -9, -1)
-BF16, FP32 = 0, 1
+BF16, FP32, FP16 = 0, 1, 2
 
 
 class FastarError(RuntimeError):
@@ -65,6 +65,12 @@ SIGNATURES = {
     "fastar_launch_count": (C.c_int64, [_vp]),
     "fastar_annca_select_noalloc": (C.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i64, _i64, _i64, _i64, _vp, _vp]),
     "fastar_noalloc_last_status": (C.c_int, [_vp]),
+    "fastar_block_tables": (C.c_int, [_vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "fastar_kv8_append": (C.c_int, [_vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp]),
+    "fastar_kv8_attention_workspace_bytes": (C.c_size_t, [_i32] * 7),
+    "fastar_kv8_attention": (C.c_int, [_vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 9 + [_vp, C.c_size_t, _vp]),
+    "fastar_packed_attention": (C.c_int, [_vp] * 4 + [_i64] * 4 + [_vp] + [_i32] * 8 + [_vp]),
+    "fastar_dense_last_status": (C.c_int, [_vp]),
     "fastar_profile_enable": (C.c_int, [_vp, _i32]),
     "fastar_profile_read": (C.c_int, [_vp, _vp, _vp, _vp]),
     "fastar_status_string": (C.c_char_p, [C.c_int]),
@@ -412,6 +418,142 @@ def annca_select_noalloc(q, k_prompt, frame_len: int, keep_tokens: int, sel_out=
 def noalloc_last_status() -> int:
     """Device status of the allocation-free selection on the current device (0 = ok); synchronises and clears it."""
     return load_library().fastar_noalloc_last_status(_stream())
+
+
+# ---- the dense path of several rollouts -----------------------------------------------------------
+# Packed sequences: tokens [cu[b], cu[b+1]) of [head][T][d] belong to sequence b.  The 8-bit cache: code pools [pages][kv heads][page tokens][d] (uint8,
+# fp8 e4m3 codes) with scales [pages][kv heads] (fp32), and a table [sequences][width] of pages.  Full rules: include/fastar.h.
+_dense_dtypes = None
+
+
+def _need(ok: bool, where: str) -> None:
+    if not ok:
+        raise FastarError(ERR_INVALID_ARG, where)
+
+
+def _rows(t, where: str):
+    """(dtype code, head stride, token stride) of a packed tensor [head][T][d]."""
+    global _dense_dtypes
+    if _dense_dtypes is None:
+        import torch
+        _dense_dtypes = {torch.bfloat16: BF16, torch.float16: FP16}
+    dtype = _dense_dtypes.get(t.dtype)
+    _need(dtype is not None and t.dim() == 3 and t.is_cuda and (t.stride(2) == 1 or t.shape[2] == 1), where)
+    return dtype, t.stride(0), t.stride(1)
+
+
+def _ints(where: str, device, *tensors) -> None:
+    import torch
+    for t in tensors:
+        _need(t.dtype == torch.int32 and t.device == device and t.is_contiguous(), where)
+
+
+class _on:
+    """The tensors' device as the current one, at no cost where it is already."""
+
+    def __init__(self, device):
+        self.device, self.guard = device, None
+
+    def __enter__(self):
+        import torch
+        if torch.cuda.current_device() != self.device.index:
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add: int) -> Dict[str, "object"]:
+    """Page tables and slots on the GPU from the requests' lengths: held, add [B] int32, the free list free_pages[first:] and table [B][W], whose new
+    entries are written in place.  Returns cu [B+1], lens [B] (-1: refused), slots [max_add] int64 and first [1], where the free list goes on."""
+    import torch
+    where, dev = "block_tables", held.device
+    _need(held.is_cuda and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and first.numel() == 1 and max_add >= 0, where)
+    _ints(where, dev, held, add, free_pages, first, table)
+    B = held.shape[0]
+    with _on(dev):
+        cu_lens = torch.empty(2 * B + 2, dtype=torch.int32, device=dev)
+        slots = torch.empty(max_add, dtype=torch.int64, device=dev)
+        r = dict(cu=cu_lens[: B + 1], lens=cu_lens[B + 1: 2 * B + 1], slots=slots, first=cu_lens[2 * B + 1:])
+        _check(load_library().fastar_block_tables(held.data_ptr(), add.data_ptr(), B, page_tokens, free_pages.data_ptr(), free_pages.numel(), first.data_ptr(),
+                                                  table.data_ptr(), table.shape[1], r["cu"].data_ptr(), r["lens"].data_ptr(), slots.data_ptr(), max_add,
+                                                  r["first"].data_ptr(), _stream()), "fastar_block_tables")
+    return r
+
+
+def _pools(where, device, k_codes, v_codes, k_scale, v_scale):
+    import torch
+    P, KV, PT, D = k_codes.shape
+    for t in (k_codes, v_codes):
+        _need(t.dtype == torch.uint8 and t.device == device and t.is_contiguous() and tuple(t.shape) == (P, KV, PT, D), where)
+    for t in (k_scale, v_scale):
+        _need(t.dtype == torch.float32 and t.device == device and t.is_contiguous() and tuple(t.shape) == (P, KV), where)
+    return P, KV, PT, D
+
+
+def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu) -> None:
+    """Writes the packed rows k_new, v_new [KV][T][d] into the 8-bit pages: token i of sequence b to position lens[b] - n_b + i."""
+    where, dev = "kv8_append", k_new.device
+    dtype, hs, ts = _rows(k_new, where)
+    _need(_rows(v_new, where) == (dtype, hs, ts) and v_new.shape == k_new.shape and v_new.device == dev, where)
+    P, KV, PT, D = _pools(where, dev, k_codes, v_codes, k_scale, v_scale)
+    B = lens.shape[0]
+    _need(k_new.shape[0] == KV and k_new.shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and tuple(cu.shape) == (B + 1,), where)
+    _ints(where, dev, table, lens, cu)
+    with _on(dev):
+        _check(load_library().fastar_kv8_append(k_new.data_ptr(), v_new.data_ptr(), hs, ts, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                                P, PT, table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, k_new.shape[1], KV, D, dtype, _stream()),
+               "fastar_kv8_append")
+
+
+def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new: int, max_len: int, frame_len: int = 1, out=None):
+    """Attention of the packed new tokens q [H][T][d] over the 8-bit cache, which holds their own keys already; n_b <= max_new, lens[b] <= max_len.
+    frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  Returns out (rows of no sequence are left as they were)."""
+    import torch
+    where, dev = "kv8_attention", q.device
+    dtype, hs, ts = _rows(q, where)
+    P, KV, PT, D = _pools(where, dev, k_codes, v_codes, k_scale, v_scale)
+    (H, T, _), B = q.shape, lens.shape[0]
+    _need(q.shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and tuple(cu.shape) == (B + 1,), where)
+    _ints(where, dev, table, lens, cu)
+    if out is None:
+        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)
+    _need(_rows(out, where) == (dtype, hs, ts) and out.shape == q.shape and out.device == dev, where)
+    lib = load_library()
+    with _on(dev):
+        nbytes = lib.fastar_kv8_attention_workspace_bytes(B, T, max_new, max_len, H, KV, D)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(lib.fastar_kv8_attention(q.data_ptr(), out.data_ptr(), hs, ts, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
+                                        table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
+                                        work.data_ptr(), nbytes, _stream()), "fastar_kv8_attention")
+    return out
+
+
+def packed_attention(q, k, v, cu, max_tokens: int, frame_len: int = 1, out=None):
+    """Attention of packed sequences over their own tokens: q [H][T][d], k and v [KV][T][d], H a multiple of KV; no sequence is longer than max_tokens.
+    frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  Returns out (rows of no sequence are left as they were)."""
+    import torch
+    where, dev = "packed_attention", q.device
+    dtype, hs, ts = _rows(q, where)
+    kd, khs, kts = _rows(k, where)
+    _need(kd == dtype and _rows(v, where) == (kd, khs, kts) and v.shape == k.shape and k.device == dev and v.device == dev, where)
+    (H, T, D), KV = q.shape, k.shape[0]
+    _need(k.shape[1] == T and k.shape[2] == D and cu.dim() == 1 and cu.shape[0] >= 2, where)
+    _ints(where, dev, cu)
+    if out is None:
+        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)
+    _need(_rows(out, where) == (dtype, hs, ts) and out.shape == q.shape and out.device == dev, where)
+    with _on(dev):
+        _check(load_library().fastar_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), hs, ts, khs, kts, cu.data_ptr(), cu.shape[0] - 1, T,
+                                                      max_tokens, H, KV, D, dtype, frame_len, _stream()), "fastar_packed_attention")
+    return out
+
+
+def dense_last_status() -> int:
+    """Device status of the dense path on the current device (0 = ok); synchronises and clears it."""
+    return load_library().fastar_dense_last_status(_stream())
 
 
 # ---- helpers for moving synthetic numpy data (bf16-exact float32) onto the device ---------------
