@@ -409,9 +409,9 @@ int fastar_block_tables(const int32_t* held, const int32_t* add, int32_t num_seq
 
 /* New rows into the cache: k_new, v_new dev [num_kv_heads][T][d].  The scale of a page and head is the least power of two s with |x| / s <= 448
  * for all its rows (2^-126 at least); codes are x / s rounded to the nearest even.  A page whose first row is written by this call starts anew;
- * in one that has rows already the scale only grows, and they are recoded (exactly, but for codes below e4m3's least normal number).  Values that
- * are not finite do not count towards the scale and become the code that is no number.  Other rows are left as they were.  A page that is written
- * belongs to one sequence of the call. */
+ * in one that has rows already the scale only grows, and its other rows are recoded then (exactly, but for codes below e4m3's least normal number).
+ * Values that are not finite do not count towards the scale and become the code that is no number.  All else is left as it was.  A page that is
+ * written belongs to one sequence of the call. */
 int fastar_kv8_append(const void* k_new, const void* v_new, int64_t head_stride, int64_t token_stride, uint8_t* k_codes, uint8_t* v_codes,
                       float* k_scale, float* v_scale, int32_t num_pages, int32_t page_tokens, const int32_t* table, int32_t table_width,
                       const int32_t* lens, const int32_t* cu, int32_t num_seqs, int32_t total_tokens, int32_t num_kv_heads, int32_t head_dim,

@@ -94,6 +94,7 @@ struct AppendArgs {
 };
 int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st);
 int launch_dense_rows(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
+int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 
 }  // namespace fastar

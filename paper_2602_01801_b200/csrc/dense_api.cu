@@ -44,6 +44,36 @@ int shape_ok(int H, int KV, int D, int dtype) {
   if (H > 65535) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   return FASTAR_OK;
 }
+// Rows of a key head and positions are counted in 32 bits.
+constexpr int64_t kMostRows = int64_t{1} << 30;
+bool too_long(int total, int max_len, int H, int KV) { return static_cast<int64_t>(total) * (H / KV) > kMostRows || max_len > kMostRows; }
+// How attention over the cache is launched: which kernels, and parts of how many keys.
+struct AttendPlan {
+  int few_rows;                    // 0: the kernel for few rows is not launched
+  bool many;
+  int chunk, parts;
+};
+constexpr int kFewRows = 32;       // two tiles of rows read the keys twice, the second time out of L2
+AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV) {
+  AttendPlan p{};
+  const int64_t G = H / KV, rows = static_cast<int64_t>(max_new) * G, len = max_len;
+  p.many = rows > kFewRows;
+  p.few_rows = kFewRows;
+  // Enough parts for four CTAs an SM, of 128 keys (a tile for each warp) at least
+  const int64_t units = static_cast<int64_t>(B) * (((rows < kFewRows ? rows : kFewRows) + 15) / 16) * KV;
+  int64_t parts = units < 592 ? 592 / units : 1;
+  const int64_t most = (len + 127) / 128;
+  if (parts > most) parts = most;
+  p.chunk = static_cast<int>(((len + parts - 1) / parts + 127) / 128 * 128);
+  p.parts = static_cast<int>((len + p.chunk - 1) / p.chunk);
+  if (p.many) {
+    p.few_rows = 0;
+    p.chunk = max_len;
+    p.parts = 1;
+  }
+  (void)T;
+  return p;
+}
 }  // namespace
 }  // namespace fastar
 
@@ -91,8 +121,13 @@ extern "C" int fastar_kv8_append(const void* k_new, const void* v_new, int64_t h
 
 extern "C" size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
                                                        int32_t num_kv_heads, int32_t head_dim) {
-  if (shape_ok(num_heads, num_kv_heads, head_dim, FASTAR_BF16) != FASTAR_OK || num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new) return 0;
-  return 16;
+  if (shape_ok(num_heads, num_kv_heads, head_dim, FASTAR_BF16) != FASTAR_OK || num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new ||
+      too_long(total_tokens, max_len, num_heads, num_kv_heads))
+    return 0;
+  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads);
+  if (p.parts == 1) return 16;
+  const size_t rows = static_cast<size_t>(p.parts) * total_tokens * num_heads;
+  return rows * (head_dim + 2) * 4 + 16;
 }
 
 extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_stride, int64_t token_stride, const uint8_t* k_codes, const uint8_t* v_codes,
@@ -105,6 +140,7 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   if (num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new || frame_len < 0 || num_pages < 1 || table_width < 1) return FASTAR_ERR_INVALID_ARG;
   if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (max_len > static_cast<int64_t>(table_width) * page_tokens) return FASTAR_ERR_INVALID_ARG;
+  if (too_long(total_tokens, max_len, num_heads, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (!table || !lens || !cu || !aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
   if (!k_codes || !v_codes || !k_scale || !v_scale || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
     return FASTAR_ERR_INVALID_ARG;
@@ -119,10 +155,18 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   a.cu = cu; a.frame = frame_len; a.max_new = max_new; a.max_len = max_len;
   a.kc = k_codes; a.vc = v_codes; a.ks = k_scale; a.vs = v_scale; a.table = table; a.lens = lens;
   a.W = table_width; a.pages = num_pages; a.PT = page_tokens;
-  a.parts = 1; a.chunk = max_len;
+  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads);
+  a.parts = p.parts; a.chunk = p.chunk; a.few_rows = p.few_rows;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<size_t>(p.parts) * total_tokens * num_heads * head_dim);
   r = dense_device(&a.status);
   if (r != FASTAR_OK) return r;
-  return launch_dense_rows(a, head_dim, dtype == FASTAR_FP16, static_cast<cudaStream_t>(stream));
+  const bool fp16 = dtype == FASTAR_FP16;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (p.few_rows > 0) r = launch_dense_few(a, head_dim, fp16, st);
+  if (r == FASTAR_OK && p.many) r = launch_dense_rows(a, head_dim, fp16, st);
+  if (r == FASTAR_OK && p.parts > 1) r = launch_dense_join(a, head_dim, fp16, st);
+  return r;
 }
 
 extern "C" int fastar_packed_attention(const void* q, const void* k, const void* v, void* out, int64_t head_stride, int64_t token_stride,
@@ -132,6 +176,7 @@ extern "C" int fastar_packed_attention(const void* q, const void* k, const void*
   int r = shape_ok(num_heads, num_kv_heads, head_dim, dtype);
   if (r != FASTAR_OK) return r;
   if (num_seqs < 1 || total_tokens < 0 || max_tokens < 1 || frame_len < 0 || !cu || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
+  if (too_long(total_tokens, max_tokens, num_heads, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (total_tokens == 0) return FASTAR_OK;
   if (!rows_ok(q, head_stride, token_stride, num_heads, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, head_dim)) return FASTAR_ERR_INVALID_ARG;
   if (!rows_ok(k, kv_head_stride, kv_token_stride, num_kv_heads, head_dim) || !rows_ok(v, kv_head_stride, kv_token_stride, num_kv_heads, head_dim))

@@ -159,7 +159,7 @@ __device__ __forceinline__ float exp2i(int e) { return __uint_as_float(static_ca
 __device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) <= 3.4028235e38f ? x : __int_as_float(0x7FC00000); }
 
 template <class T, int D>
-__device__ __forceinline__ void append_rows(const T* __restrict__ src, int64_t ts, int rows, int row0, bool fresh, uint8_t* page, float* scale, uint32_t* red) {
+__device__ __forceinline__ void append_rows(const T* __restrict__ src, int64_t ts, int rows, int row0, int page_rows, bool fresh, uint8_t* page, float* scale, uint32_t* red) {
   constexpr int TPR = D / 16, RPP = kAppendThreads / TPR, MAXP = 128 / RPP;      // threads a row, rows a pass
   const int c = threadIdx.x % TPR, r0 = threadIdx.x / TPR;
   uint4 x[MAXP][2];
@@ -205,9 +205,10 @@ __device__ __forceinline__ void append_rows(const T* __restrict__ src, int64_t t
       }
     *reinterpret_cast<uint4*>(page + (row0 + r) * D + c * 16) = make_uint4(o[0], o[1], o[2], o[3]);
   }
-  if (!fresh && was < to) {              // the rows that are there already
+  if (!fresh && was < to) {              // the page's other rows
     const float f = was * inv;
-    for (int r = r0; r < row0; r += RPP) {
+    for (int r = r0; r < page_rows; r += RPP) {
+      if (r >= row0 && r < row0 + rows) continue;
       uint4* at = reinterpret_cast<uint4*>(page + r * D + c * 16);
       uint4 v = *at;
 #pragma unroll
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const Append
   const int lo = max(past, i * a.PT), rows = min(len - i * a.PT, a.PT) - (lo - i * a.PT), row0 = lo - i * a.PT;
   const int64_t at = static_cast<int64_t>(page) * a.KV + kvh, src = kvh * a.hs + (t0 + lo - past) * a.ts;
   const bool v = blockIdx.z != 0;
-  append_rows<T, D>(static_cast<const T*>(v ? a.v : a.k) + src, a.ts, rows, row0, row0 == 0, (v ? a.vc : a.kc) + at * a.PT * D, (v ? a.vs : a.ks) + at, most);
+  append_rows<T, D>(static_cast<const T*>(v ? a.v : a.k) + src, a.ts, rows, row0, a.PT, row0 == 0, (v ? a.vc : a.kc) + at * a.PT * D, (v ? a.vs : a.ks) + at, most);
 }
 
 int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st) {

@@ -51,8 +51,7 @@ def append(x, codes, scale, table, lens, cu, values):
                 least = scale_of(float(torch.where(fine, rows, 0.0).abs().max()))
                 to = least if lo == i * PT else max(least, float(sc[page, h]))
                 if lo > i * PT and to > float(sc[page, h]):
-                    r = slice(0, lo - i * PT)
-                    val[page, h, r] = e4m3_codes(val[page, h, r] * (float(sc[page, h]) / to))
+                    val[page, h] = e4m3_codes(val[page, h] * (float(sc[page, h]) / to))
                 new = torch.where(fine, e4m3_codes(torch.where(fine, rows, 0.0) / to), float("nan"))
                 val[page, h, lo - i * PT: hi - i * PT] = new
                 sc[page, h] = to

@@ -341,7 +341,7 @@ def run_append(fastar, dtype, D, KV, PT, steps, seed=1, layout="htd", scale_of_s
         k, v = (rows(g, KV, cu[-1] + 3, D, dt, layout, scale_of_step(s)) for _ in range(2))
         if spoil is not None:
             spoil(s, k, v)
-        before = [c.clone() for c in pool.codes]
+        before, was = [c.clone() for c in pool.codes], [c.clone() for c in pool.scale]
         want = [R.append(x, c, sc, table, lens, cu, values[c.long()]) for x, c, sc in zip((k, v), pool.codes, pool.scale)]
         fastar.kv8_append(k, v, *pool.args(), table, i32(lens), i32(cu))
         for w in range(2):
@@ -350,11 +350,12 @@ def run_append(fastar, dtype, D, KV, PT, steps, seed=1, layout="htd", scale_of_s
             assert torch.equal(torch.nan_to_num(pool.scale[w].double(), nan=-1.0), torch.nan_to_num(sc, nan=-1.0))
             assert torch.equal(torch.isnan(got), torch.isnan(val))
             assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(val))
-            # bytes of rows that hold nothing are as they were
+            # bytes of rows that hold nothing are as they were, but in a page that has been recoded
             mask = torch.ones(pool.pages, PT, dtype=torch.bool, device=DEV)
             for b in range(B):
                 for i in range(-(-lens[b] // PT)):
                     mask[int(table[b, i]), : min(PT, lens[b] - i * PT)] = False
+            mask[(pool.scale[w] != was[w]).any(1)] = False
             same = (pool.codes[w] == before[w]).all(-1).all(1)
             assert bool(same[mask].all())
 
