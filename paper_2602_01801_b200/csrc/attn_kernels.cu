@@ -96,27 +96,6 @@ __device__ __forceinline__ float lds1(uint32_t addr) {
   asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
   return v;
 }
-// 2^u of two logits on the FMA units, u < 2^22; 0 from -127 down, as the special-function units give it for a logit of -inf.  Adding 1.5 x 2^23
-// rounds u to the nearest integer, which goes to the exponent; 2^f of the rest, on [-1/2, 1/2], by a polynomial of degree 5 fitted to the least
-// relative error with 2^0 = 1.  Error 1.1e-7 at most, 1.7e-7 as worked out in fp32 (ex2.approx 1.2e-7); rounding to bf16 is 2e-3.
-__device__ __forceinline__ float2 poly_exp2(float2 u) {
-  auto both = [](float v) { return make_float2(v, v); };
-  constexpr float kRound = 12582912.f;                     // 1.5 x 2^23: the sum's last bits are the nearest integer
-  u.x = fmaxf(u.x, -127.f);
-  u.y = fmaxf(u.y, -127.f);
-  const float2 r = fadd2(u, both(kRound)), f = ffma2(fadd2(r, both(-kRound)), both(-1.f), u);
-  float2 y = both(0x1.5bba14p-10f);
-  y = ffma2(y, f, both(0x1.3cea88p-7f));
-  y = ffma2(y, f, both(0x1.c6b752p-5f));
-  y = ffma2(y, f, both(0x1.ebf9bcp-3f));
-  y = ffma2(y, f, both(0x1.62e42ap-1f));
-  y = ffma2(y, f, both(1.f));
-  return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(r.x) << 23)), __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(r.y) << 23)));
-}
-// Both halves of a bf16 pair to a sum each, as they are.
-__device__ __forceinline__ void add_bf16x2(float2& s, uint32_t b) {
-  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.bf16 %0, l, %0; add.f32.bf16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
-}
 // Flat items.  What a logit can be at most follows from |q| and from the bounds that the cache keeps for the blocks of an item (BlockBound) and
 // that come with a segment.  If that, for the rows of a warp, is not more than kTop above the reference that an item's first sub-tile gives,
 // nothing after it can ask for another reference: the sub-tiles that follow need no maximum, no look at the others' and no hand-over, which are

@@ -1,6 +1,7 @@
 // The dense path of several rollouts (fastar_block_tables, fastar_kv8_append, fastar_kv8_attention, fastar_packed_attention): what its kernels
 // share, and the index arithmetic that runs on the host too.
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -93,7 +94,7 @@ struct AppendArgs {
   int32_t* status;
 };
 int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st);
-int launch_dense_rows(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
+int launch_dense_many(const DenseArgs& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int D, bool fp16, cudaStream_t st);
 int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 

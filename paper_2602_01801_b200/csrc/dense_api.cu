@@ -14,6 +14,7 @@ static __device__ int32_t g_dense_status;
 namespace {
 std::mutex g_dense_mu;
 int32_t* g_dense_word[64] = {};
+PFN_cuTensorMapEncodeTiled_v12000 g_dense_encode = nullptr;
 
 int dense_device(int32_t** status) {
   int dev = -1;
@@ -24,6 +25,12 @@ int dense_device(int32_t** status) {
     int major = 0;
     if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return FASTAR_ERR_CUDA;
     if (major != 10) return FASTAR_ERR_NOT_SM100;
+    if (!g_dense_encode) {
+      void* fn = nullptr;
+      cudaDriverEntryPointQueryResult q;
+      if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || !fn || q != cudaDriverEntryPointSuccess) return FASTAR_ERR_CUDA;
+      g_dense_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    }
     void* p = nullptr;
     if (cudaGetSymbolAddress(&p, g_dense_status) != cudaSuccess || !p) return FASTAR_ERR_CUDA;
     g_dense_word[dev] = static_cast<int32_t*>(p);
@@ -47,31 +54,49 @@ int shape_ok(int H, int KV, int D, int dtype) {
 // Rows of a key head and positions are counted in 32 bits.
 constexpr int64_t kMostRows = int64_t{1} << 30;
 bool too_long(int total, int max_len, int H, int KV) { return static_cast<int64_t>(total) * (H / KV) > kMostRows || max_len > kMostRows; }
-// How attention over the cache is launched: which kernels, and parts of how many keys.
+// Tiles of 128 tokens x 64 columns of a packed tensor [heads][T][d].
+int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int heads, int64_t ts, int64_t hs, bool fp16) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(tokens), static_cast<cuuint64_t>(heads)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ts) * 2, static_cast<cuuint64_t>(heads == 1 ? ts : hs) * 2};      // (one head: its stride is not used)
+  const cuuint32_t box[3] = {64, 128, 1}, estr[3] = {1, 1, 1};
+  return g_dense_encode(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? FASTAR_OK
+             : FASTAR_ERR_CUDA;
+}
+
+// How attention over the cache is launched: which kernels, and parts of how many keys (a multiple of 128).
 struct AttendPlan {
   int few_rows;                    // 0: the kernel for few rows is not launched
   bool many;
   int chunk, parts;
 };
 constexpr int kFewRows = 32;       // two tiles of rows read the keys twice, the second time out of L2
+constexpr int kSms = 148;
 AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV) {
   AttendPlan p{};
-  const int64_t G = H / KV, rows = static_cast<int64_t>(max_new) * G, len = max_len;
+  const int64_t G = H / KV, rows = static_cast<int64_t>(max_new) * G, len = max_len, tiles = (len + 127) / 128;
   p.many = rows > kFewRows;
-  p.few_rows = kFewRows;
-  // Enough parts for four CTAs an SM, of 128 keys (a tile for each warp) at least
-  const int64_t units = static_cast<int64_t>(B) * (((rows < kFewRows ? rows : kFewRows) + 15) / 16) * KV;
-  int64_t parts = units < 592 ? 592 / units : 1;
-  const int64_t most = (len + 127) / 128;
-  if (parts > most) parts = most;
+  const bool equal = static_cast<int64_t>(B) * max_new <= T;       // the sequences may all be that long; if they are not, the kernel for many rows serves them too
+  p.few_rows = p.many && equal ? 0 : kFewRows;
+  int64_t parts = 1;
+  if (!p.many) {
+    // enough parts for four CTAs an SM, of 128 keys (a tile for each warp) at least
+    const int64_t units = static_cast<int64_t>(B) * ((rows + 15) / 16) * KV;
+    if (units < 4 * kSms) parts = 4 * kSms / units;
+    if (parts > tiles) parts = tiles;
+  } else {
+    // One CTA an SM: the parts that take the fewest rounds x (key tiles + 3, what a CTA takes to begin and end), with three more for the join
+    const int64_t ctas = ((static_cast<int64_t>(T) * G + 255) / 256) * KV;
+    int64_t best = INT64_MAX;
+    for (int64_t k = 1; k <= 64 && k * 4 <= tiles + 3; ++k) {
+      const int64_t cost = (ctas * k + kSms - 1) / kSms * ((tiles + k - 1) / k + 3) + (k > 1 ? 3 : 0);
+      if (cost < best) { best = cost; parts = k; }
+      if (ctas * k > 8 * kSms) break;
+    }
+  }
   p.chunk = static_cast<int>(((len + parts - 1) / parts + 127) / 128 * 128);
   p.parts = static_cast<int>((len + p.chunk - 1) / p.chunk);
-  if (p.many) {
-    p.few_rows = 0;
-    p.chunk = max_len;
-    p.parts = 1;
-  }
-  (void)T;
   return p;
 }
 }  // namespace
@@ -164,7 +189,7 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   const bool fp16 = dtype == FASTAR_FP16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (p.few_rows > 0) r = launch_dense_few(a, head_dim, fp16, st);
-  if (r == FASTAR_OK && p.many) r = launch_dense_rows(a, head_dim, fp16, st);
+  if (r == FASTAR_OK && p.many) r = launch_dense_many(a, CUtensorMap{}, CUtensorMap{}, head_dim, fp16, st);
   if (r == FASTAR_OK && p.parts > 1) r = launch_dense_join(a, head_dim, fp16, st);
   return r;
 }
@@ -189,7 +214,12 @@ extern "C" int fastar_packed_attention(const void* q, const void* k, const void*
   a.parts = 1; a.chunk = max_tokens;
   r = dense_device(&a.status);
   if (r != FASTAR_OK) return r;
-  return launch_dense_rows(a, head_dim, dtype == FASTAR_FP16, static_cast<cudaStream_t>(stream));
+  const bool fp16 = dtype == FASTAR_FP16;
+  CUtensorMap tm_k, tm_v;
+  r = encode_packed(&tm_k, k, head_dim, total_tokens, num_kv_heads, kv_token_stride, kv_head_stride, fp16);
+  if (r == FASTAR_OK) r = encode_packed(&tm_v, v, head_dim, total_tokens, num_kv_heads, kv_token_stride, kv_head_stride, fp16);
+  if (r != FASTAR_OK) return r;
+  return launch_dense_many(a, tm_k, tm_v, head_dim, fp16, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int fastar_dense_last_status(void* stream) {

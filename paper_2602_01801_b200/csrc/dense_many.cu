@@ -1,0 +1,588 @@
+// Dense attention for sequences with many rows: packed prompts over their own keys (TMA), and chunks over the 8-bit cache (codes converted on the way).
+//
+// The rows of a key head are (token, query head) pairs, token-major, so that G query heads that share keys share their tiles, and a causal limit moves by one
+// every G rows.  A CTA takes 256 of them as two query tiles of 128 (TMEM lanes) and walks the key tiles of 128:
+//   S_t  = Q_t K_j^T              tcgen05.mma, shared memory x shared memory -> TMEM
+//   P_t  = exp2(S_t f - m)        a thread a row; P_t takes the place of S_t's first half in TMEM
+//   O_t += P_t V_j                tcgen05.mma, TMEM x shared memory
+// While one tile is in its exponentials the tensor core has the other's products: 2 x 1 060 cycles of MMAs against 2 x 1 024 of the special-function units per
+// key tile, so an eighth of the exponentials goes to the FMA units.  The running maximum is raised only when a logit exceeds it by 8 binary orders (O is
+// rescaled then, by the warps that own its rows); sums add up the probabilities as rounded.
+// 8-bit cache: four warps read codes, convert them to fp16 (exact) and put them where TMA would have put them.  Queries are fp16 too, their row divided by a
+// power of two; a page's key scale goes into the factor of the logits, value scales are taken relative to the largest of the CTA's keys (a power of two, so
+// nothing is rounded within 2^15 of it; beyond that, and where there are NaN codes, the rows are worked out from the definition).
+// What a row does not see must not reach it: V rows behind the last visible key are zeroed, and values that are not finite in a tile that some row does not see as
+// a whole are taken out, and all rows of the CTA are worked out from the definition afterwards (dense_rows.cuh).
+// Warp roles: 0-3 and 4-7 soft-max of the two tiles, 8-11 Q, and the codes' way in (or the look at V), 12 MMAs, 13 K, 14 V (TMA).
+#include <cudaTypedefs.h>
+
+#include "common.h"
+#include "dense.h"
+#include "dense_rows.cuh"
+
+namespace fastar {
+
+constexpr int kManyThreads = 512, kMoveWarp = 8, kMmaWarp = 12, kKWarp = 13, kVWarp = 14;
+constexpr int kRowsCta = 256, kKeys = 128;
+// Registers a thread, dealt anew by role: 512 x 128 at launch = 256 x 184 + 128 x 96 + 128 x 48
+constexpr int kSoftmaxRegs = 184, kMoveRegs = 96, kRestRegs = 48;
+constexpr float kRaise = 8.f;
+
+template <int D>
+struct ManySmem {
+  static constexpr int q_tile = (D / 64) * 128 * 128;              // bytes of a query tile, and of a K or V tile
+  static constexpr int SK = D == 128 ? 3 : 4, SV = D == 128 ? 2 : 4;
+  static constexpr int k_off = 2 * q_tile, v_off = k_off + SK * q_tile, bar_off = v_off + SV * q_tile;
+  static constexpr int scale_off = bar_off + 256;                  // [8][2] key scales of a tile's two halves
+  static constexpr int misc_off = scale_off + 64;
+  static constexpr int factor_off = misc_off + 64;                 // [256]
+  static constexpr int total = factor_off + 1024;
+  static_assert(total <= 227 * 1024, "shared memory");
+};
+
+struct ManyItem {
+  int b, kvh, part, row0, rows;                                    // rows of the sequence, first of the CTA
+  int past, k0;
+  int nt[2], whole_from[2];                                        // key tiles of the query tiles; from which tile on some row does not see all of it
+  int see;                                                         // end of the keys that any row sees
+};
+
+__host__ __device__ constexpr uint32_t make_idesc_f16(int m, int n, int b_mn_major) {
+  return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+__device__ __forceinline__ void add_f16x2(float2& s, uint32_t b) {
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.f16 %0, l, %0; add.f32.f16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// Place of a 16-byte piece of a row in a tile of 128 rows (128-byte swizzle, 64 columns of 16 bits a chunk).
+__device__ __forceinline__ uint32_t tile_at16(int row, int piece) { return (piece >> 3) * 16384 + row * 128 + (((piece & 7) ^ (row & 7)) << 4); }
+
+template <class T, int D, bool PAGED>
+__global__ void __launch_bounds__(kManyThreads, 1)
+many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const DenseArgs a) {
+  using SM = ManySmem<D>;
+  using M = typename std::conditional<PAGED, __half, T>::type;     // the products' type
+  constexpr bool kHalf = std::is_same<M, __half>::value;
+  constexpr int SK = SM::SK, SV = SM::SV;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  if (sbase & 1023u) {
+    if (threadIdx.x == 0 && a.status) record_status(a.status, FASTAR_ERR_CUDA);
+    return;
+  }
+  const uint32_t bar = sbase + SM::bar_off;
+  const uint32_t bar_q = bar, bar_k_full = bar + 8, bar_k_empty = bar_k_full + 8 * SK, bar_v_full = bar_k_empty + 8 * SK, bar_v_empty = bar_v_full + 8 * SV;
+  const uint32_t bar_v_clean = bar_v_empty + 8 * SV, bar_v_asked = bar_v_clean + 8 * SV, bar_s = bar_v_asked + 8 * SV, bar_p = bar_s + 16, bar_pv = bar_p + 16;
+  const uint32_t bar_drain = bar_pv + 16;
+  constexpr int kNumBars = 1 + 2 * SK + 4 * SV + 7;
+  static_assert(kNumBars * 8 <= 256, "barriers");
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::misc_off);
+  volatile int* spoilt_s = abort_flag + 1;
+  volatile int* done_flag = abort_flag + 2;                        // stays 0
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + SM::misc_off + 12);
+  volatile float* unit_s = reinterpret_cast<volatile float*>(smem + SM::misc_off + 16);        // [4] by mover warp
+  volatile int* item_s = reinterpret_cast<volatile int*>(smem + SM::misc_off + 32);           // sequence, tile of it
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  chain_wait();
+
+  // ---- the item: tiles of the sequences in order, a sequence's last (longest) first
+  {
+    int* red = reinterpret_cast<int*>(smem);                       // 17 words
+    const int tile = blockIdx.x / a.KV;
+    int64_t before = 0;
+    if (threadIdx.x == 0) {
+      item_s[0] = -1;
+      *abort_flag = *spoilt_s = *done_flag = 0;
+    }
+    for (int b0 = 0; b0 < a.B && before <= tile; b0 += kManyThreads) {
+      const int b = b0 + threadIdx.x;
+      int mine = 0;
+      if (b < a.B) {
+        DenseSeq s;
+        const int r = seq_of(a, b, s);
+        if (r < 0 && a.status) record_status(a.status, kErrBounds);
+        const int rows = s.n * a.G;
+        if (r > 0 && rows > a.few_rows) mine = (rows + kRowsCta - 1) / kRowsCta;
+      }
+      int x = mine;
+#pragma unroll
+      for (int w = 1; w < 32; w <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, x, w);
+        if (lane >= w) x += u;
+      }
+      if (lane == 31) red[warp] = x;
+      __syncthreads();
+      int off = 0, all = 0;
+#pragma unroll
+      for (int w = 0; w < kManyThreads / 32; ++w) {
+        if (w < warp) off += red[w];
+        all += red[w];
+      }
+      const int64_t first = before + off + x - mine;
+      if (mine > 0 && tile >= first && tile < first + mine) {
+        item_s[0] = b;
+        item_s[1] = mine - 1 - static_cast<int>(tile - first);
+      }
+      before += all;
+      __syncthreads();
+    }
+  }
+  ManyItem it;
+  it.b = item_s[0];
+  if (it.b < 0) return;
+  DenseSeq s;
+  seq_of(a, it.b, s);
+  it.kvh = blockIdx.x % a.KV;
+  it.part = blockIdx.y;
+  const bool whole = a.parts == 1 || s.len <= a.chunk;
+  if (whole ? it.part > 0 : static_cast<int64_t>(it.part) * a.chunk >= s.len) return;
+  it.rows = s.n * a.G;
+  it.row0 = item_s[1] * kRowsCta;
+  it.past = s.len - s.n;
+  it.k0 = whole ? 0 : it.part * a.chunk;
+  it.see = 0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r0 = it.row0 + 128 * t, r1 = min(it.rows, r0 + 128) - 1;
+    int any = r0 < it.rows ? visible_end(it.past + r1 / a.G, s.len, a.frame) : 0;
+    if (!whole) any = min(any, it.k0 + a.chunk);
+    const int all = r0 < it.rows ? visible_end(it.past + r0 / a.G, s.len, a.frame) : 0;
+    it.nt[t] = any > it.k0 ? (any - it.k0 + kKeys - 1) / kKeys : 0;
+    it.whole_from[t] = all > it.k0 ? (all - it.k0) / kKeys : 0;
+    it.see = max(it.see, any);
+  }
+  const int nt = max(it.nt[0], it.nt[1]);
+  const int clean_from = it.nt[1] > 0 ? (it.nt[0] > 0 ? min(it.whole_from[0], it.whole_from[1]) : it.whole_from[1]) : it.whole_from[0];
+
+  if (threadIdx.x < kNumBars) {
+    const int i = threadIdx.x;
+    // q; k_full, k_empty; v_full, v_empty, v_clean, v_asked; s, p, pv (two each), drain
+    const int count = i == 0 ? 4 : i < 1 + SK ? (PAGED ? 4 : 1) : i < 1 + 2 * SK ? 1 : i < 1 + 2 * SK + SV ? (PAGED ? 4 : 1) : i < 1 + 2 * SK + 2 * SV ? 1
+                      : i < 1 + 2 * SK + 3 * SV ? 4 : i < 1 + 2 * SK + 4 * SV ? 1 : i < 3 + 2 * SK + 4 * SV ? 2 : i < 5 + 2 * SK + 4 * SV ? 4 : 1;
+    mbar_init(bar + 8 * i, count);
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  if (!PAGED && warp == kKWarp && lane == 0) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp >= kMmaWarp) {
+    setmaxnreg_dec<kRestRegs>();
+    if (warp == kMmaWarp) {
+      // ================================================================ MMAs
+      const uint32_t lead = elect_lane();
+      constexpr uint32_t id_s = kHalf ? make_idesc_f16(128, kKeys, 0) : make_idesc_bf16(128, kKeys, 0);
+      constexpr uint32_t id_o = kHalf ? make_idesc_f16(128, D, 1) : make_idesc_bf16(128, D, 1);
+      const uint64_t qd = make_smem_desc(sbase, 16, 1024), kd = make_smem_desc(sbase + SM::k_off, 16, 1024), vd = make_smem_desc(sbase + SM::v_off, 16384, 1024);
+      bool ok = nt > 0 && mbar_wait_warp<kIssueWaitHintNs>(bar_q, 0, abort_flag, a.status);
+      auto scores = [&](int t, int j) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
+          umma_ss(tmem + t * 128, qd + ((t * SM::q_tile) >> 4) + off, kd + (((j % SK) * SM::q_tile) >> 4) + off, id_s, k != 0, lead);
+        }
+        umma_commit(bar_s + 8 * t, lead);
+        if (lead) mbar_arrive(bar_s + 8 * t);                      // what this warp has seen arrive (key scales) is there for those who wait
+      };
+      if (ok) ok = mbar_wait_warp<kIssueWaitHintNs>(bar_k_full, 0, abort_flag, a.status);
+      if (ok) {
+        tc_fence_after();
+        for (int t = 0; t < 2; ++t)
+          if (it.nt[t] > 0) scores(t, 0);
+        umma_commit(bar_k_empty, lead);
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        const int sk = (j + 1) % SK, sv = j % SV;
+        ok = mbar_wait_warp<kIssueWaitHintNs>(bar_v_full + 8 * sv, (j / SV) & 1, abort_flag, a.status);
+        if (!PAGED && j >= clean_from) ok = ok && mbar_wait_warp(bar_v_clean + 8 * sv, ((j - clean_from) / SV) & 1, abort_flag, a.status);
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (j >= it.nt[t]) continue;
+          ok = mbar_wait_warp(bar_p + 8 * t, j & 1, abort_flag, a.status);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k)
+            umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, vd + ((sv * SM::q_tile + k * 2048) >> 4), id_o, (j | k) != 0, lead);
+          umma_commit(bar_pv + 8 * t, lead);
+          if (j + 1 < it.nt[t]) {
+            ok = mbar_wait_warp<kIssueWaitHintNs>(bar_k_full + 8 * sk, ((j + 1) / SK) & 1, abort_flag, a.status);
+            if (!ok) break;
+            tc_fence_after();
+            scores(t, j + 1);
+          }
+        }
+        if (!ok) break;
+        if (j + 1 < nt) umma_commit(bar_k_empty + 8 * sk, lead);
+        umma_commit(bar_v_empty + 8 * sv, lead);
+      }
+      umma_commit(bar_drain, lead);                                // nothing is in flight when tensor memory goes back
+      mbar_wait_warp(bar_drain, 0, done_flag, a.status);
+    } else if (!PAGED && (warp == kKWarp || warp == kVWarp)) {
+      // ================================================================ K or V tiles by TMA
+      const bool is_k = warp == kKWarp;
+      const int stages = is_k ? SK : SV;
+      const uint32_t full = is_k ? bar_k_full : bar_v_full, empty = is_k ? bar_k_empty : bar_v_empty, ring = sbase + (is_k ? SM::k_off : SM::v_off);
+      const CUtensorMap* tm = is_k ? &tm_k : &tm_v;
+      int copied = 0;
+      for (int j = 0; j < nt; ++j) {
+        const int st = j % stages;
+        if (j >= stages && !mbar_wait_warp<kIssueWaitHintNs>(empty + 8 * st, (j / stages - 1) & 1, abort_flag, a.status)) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(full + 8 * st, SM::q_tile);
+          for (int kc = 0; kc < D / 64; ++kc) tma_load_3d(ring + st * SM::q_tile + kc * 16384, tm, full + 8 * st, kc * 64, s.t0 + it.k0 + j * kKeys, it.kvh);
+          if (!is_k && j >= clean_from) mbar_arrive(bar_v_asked + 8 * st);
+        }
+        ++copied;
+      }
+      for (int j = max(0, copied - stages); j < copied; ++j) mbar_wait_warp(full + 8 * (j % stages), (j / stages) & 1, done_flag, a.status);      // all copies have landed
+    }
+  } else if (warp >= kMoveWarp) {
+    setmaxnreg_dec<kMoveRegs>();
+    const int tid = threadIdx.x - kMoveWarp * 32;
+    // ================================================================ queries
+    const T* q = static_cast<const T*>(a.q);
+    if constexpr (!PAGED) {
+      constexpr int PPR = D / 8, RPP = 128 / PPR;                  // 16-byte pieces a row, rows a pass
+      const int piece = tid % PPR;
+#pragma unroll 4
+      for (int row = tid / PPR; row < kRowsCta; row += RPP) {
+        const int r = it.row0 + row;
+        const bool live = r < it.rows;
+        const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
+        cp_async16(sbase + (row >> 7) * SM::q_tile + tile_at16(row & 127, piece), q + head * a.q_hs + (s.t0 + i) * a.q_ts + piece * 8, live);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    } else {
+      float* factor = reinterpret_cast<float*>(smem + SM::factor_off);
+#pragma unroll 1
+      for (int row = tid; row < kRowsCta; row += 128) {            // a thread a row: its largest, then fp16
+        const int r = it.row0 + row;
+        const bool live = r < it.rows;
+        const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
+        const uint4* src = reinterpret_cast<const uint4*>(q + head * a.q_hs + (s.t0 + i) * a.q_ts);
+        uint32_t most = 0;
+#pragma unroll 4
+        for (int p = 0; p < D / 8; ++p) {
+          const uint4 v = live ? __ldg(src + p) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = widen2<T>((&v.x)[e]);
+            most = max(most, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+          }
+        }
+        int e = static_cast<int>(most >> 23) - 127;
+        e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        factor[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (rsqrtf(static_cast<float>(D)) * 1.4426950408889634f);
+#pragma unroll 4
+        for (int p = 0; p < D / 8; ++p) {
+          uint4 v = live ? __ldg(src + p) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2 f = widen2<T>((&v.x)[w]);
+            (&v.x)[w] = narrow2<__half>(f.x * down, f.y * down);
+          }
+          sts128(sbase + (row >> 7) * SM::q_tile + tile_at16(row & 127, p), v);
+        }
+      }
+    }
+    fence_proxy_async_smem();
+    mbar_arrive_warp(bar_q);
+    bool spoilt = false;
+    if constexpr (!PAGED) {
+      // ================================================================ V of tiles that some row does not see as a whole
+      for (int j = clean_from; j < nt; ++j) {
+        const int st = j % SV;
+        // (a parity tells two phases apart: the copy before this one into the stage is through once this one has been asked for)
+        if (!mbar_wait_warp<kIssueWaitHintNs>(bar_v_asked + 8 * st, ((j - clean_from) / SV) & 1, abort_flag, a.status)) break;
+        if (!mbar_wait_warp<kIssueWaitHintNs>(bar_v_full + 8 * st, (j / SV) & 1, abort_flag, a.status)) break;
+        const uint32_t tile = sbase + SM::v_off + st * SM::q_tile;
+        const bool gone = it.k0 + j * kKeys + tid >= it.see;
+        constexpr uint32_t kExp = kHalf ? 0x7C00u : 0x7F80u;
+#pragma unroll 4
+        for (int p = 0; p < D / 8; ++p) {
+          const uint32_t at = tile + tile_at16(tid, p);
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          bool change = gone;
+          if (!gone) {
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              uint32_t& u = (&v.x)[w];
+              if ((u & kExp) == kExp) { u &= 0xFFFF0000u; change = spoilt = true; }
+              if ((u & (kExp << 16)) == kExp << 16) { u &= 0xFFFFu; change = spoilt = true; }
+            }
+          }
+          if (change) sts128(at, v);
+        }
+        fence_proxy_async_smem();
+        mbar_arrive_warp(bar_v_clean + 8 * st);
+      }
+    } else {
+      // ================================================================ codes -> fp16 tiles
+      const int n_pages = pages_of(s.len, a.PT), p_first = it.k0 / a.PT, p_end = it.see > it.k0 ? (it.see - 1) / a.PT + 1 : p_first;
+      // the largest value scale of the keys, in which the values are taken
+      float most = 1.17549435e-38f;
+      for (int p = p_first + tid; p < p_end; p += 128) most = fmaxf(most, a.vs[static_cast<int64_t>(page_of(a, it.b, p)) * a.KV + it.kvh]);
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+      if (lane == 0) unit_s[warp - kMoveWarp] = most;
+      named_barrier_sync(1, 128);
+      most = fmaxf(fmaxf(unit_s[0], unit_s[1]), fmaxf(unit_s[2], unit_s[3]));
+      // Units of work: K(0), then K(j + 1) and V(j) in turn.  The codes of the next one are on their way while one is converted.
+      constexpr int TPR = D / 16, RPP = 128 / TPR, PASSES = 128 / RPP;           // threads a row, rows a pass
+      const int c = tid % TPR, r0 = tid / TPR;
+      int window = -64, window_page = 0;
+      __half2 nan_seen = __float2half2_rn(0.f);
+      auto unit_of = [&](int u, bool& is_v, int& j) {              // false: past the end
+        is_v = u > 0 && (u & 1) == 0;
+        j = u == 0 ? 0 : is_v ? u / 2 - 1 : (u + 1) / 2;
+        return j < nt;
+      };
+      const int units = 2 * nt + 1;                                // (K(nt) is none)
+      auto ask = [&](int u, uint4 (&raw)[PASSES], float2& scale) {
+        bool is_v;
+        int j;
+        if (u >= units || !unit_of(u, is_v, j)) return;
+        const int key0 = it.k0 + j * kKeys;
+        const int p0 = key0 / a.PT, p1 = a.PT == 64 && key0 + 64 < it.see ? p0 + 1 : p0;
+        if (p1 - window >= 32 || window < 0 || p0 < window) {
+          window = p0;
+          window_page = p0 + lane < n_pages ? page_of(a, it.b, p0 + lane) : 0;
+        }
+        const int64_t at0 = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p0 - window)) * a.KV + it.kvh;
+        const int64_t at1 = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p1 - window)) * a.KV + it.kvh;
+        const uint8_t* codes = is_v ? a.vc : a.kc;
+        const float* scales = is_v ? a.vs : a.ks;
+        scale = make_float2(scales[at0], scales[at1]);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+          const int row = p * RPP + r0;
+          const bool second = a.PT == 64 && row >= 64;
+          const int64_t off = ((second ? at1 : at0) * a.PT + (second ? row - 64 : row)) * D + c * 16;
+          raw[p] = key0 + row < it.see ? __ldg(reinterpret_cast<const uint4*>(codes + off)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+      };
+      auto convert = [&](int u, const uint4 (&raw)[PASSES], float2 scale) {
+        bool is_v;
+        int j;
+        if (!unit_of(u, is_v, j)) return true;
+        const int st = is_v ? j % SV : j % SK, n = is_v ? SV : SK;
+        const uint32_t full = (is_v ? bar_v_full : bar_k_full) + 8 * st, empty = (is_v ? bar_v_empty : bar_k_empty) + 8 * st;
+        if (j >= n && !mbar_wait_warp<kIssueWaitHintNs>(empty, (j / n - 1) & 1, abort_flag, a.status)) return false;
+        const uint32_t tile = sbase + (is_v ? SM::v_off : SM::k_off) + st * SM::q_tile;
+        const float f0 = is_v ? scale.x / most : 1.f, f1 = is_v ? scale.y / most : 1.f;
+        if (is_v) {
+          // (2^-126 is the scale of a page of zeros)
+          if ((f0 < 3.0517578e-5f && scale.x > 1.17549435e-38f) || (f1 < 3.0517578e-5f && scale.y > 1.17549435e-38f)) spoilt = true;
+        }
+        const __half2 h0 = __float2half2_rn(f0), h1 = __float2half2_rn(f1);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+          const int row = p * RPP + r0;
+          const __half2 f = a.PT == 64 && row >= 64 ? h1 : h0;
+          uint32_t o[8];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t v = (&raw[p].x)[w];
+            o[2 * w] = e4m3x2_to_half2(v & 0xFFFFu);
+            o[2 * w + 1] = e4m3x2_to_half2(v >> 16);
+          }
+#pragma unroll
+          for (int w = 0; w < 8; ++w) {
+            __half2& h = *reinterpret_cast<__half2*>(&o[w]);
+            nan_seen = __hmax2_nan(nan_seen, h);
+            if (is_v) h = __hmul2(h, f);
+          }
+          const int first = D == 128 ? c >> 2 : 0;                 // which of its two pieces a thread stores first: eight lanes, eight banks
+          const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
+          sts128(tile + tile_at16(row, 2 * c + first), first ? hi : lo);
+          sts128(tile + tile_at16(row, 2 * c + 1 - first), first ? lo : hi);
+        }
+        if (!is_v && tid == 0) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sbase + SM::scale_off + (j & 7) * 8), "f"(scale.x), "f"(scale.y) : "memory");
+        fence_proxy_async_smem();
+        mbar_arrive_warp(full);
+        return true;
+      };
+      uint4 ra[PASSES], rb[PASSES];
+      float2 sa = make_float2(0.f, 0.f), sb = make_float2(0.f, 0.f);
+      if (nt > 0) {
+        ask(0, ra, sa);
+        for (int u = 0; u < units; u += 2) {
+          ask(u + 1, rb, sb);
+          if (!convert(u, ra, sa)) break;
+          ask(u + 2, ra, sa);
+          if (u + 1 < units && !convert(u + 1, rb, sb)) break;
+        }
+      }
+      spoilt |= __hisnan(__low2half(nan_seen)) || __hisnan(__high2half(nan_seen));
+    }
+    if (spoilt) *spoilt_s = 1;
+  } else {
+    // ================================================================== soft-max of query tile t, a thread a row
+    setmaxnreg_inc<kSoftmaxRegs>();
+    const int t = warp >> 2, row = t * 128 + (threadIdx.x & 127), r = it.row0 + row, n = it.nt[t];
+    const bool live = r < it.rows;
+    const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
+    const int end = live ? visible_end(it.past + i, s.len, a.frame) - it.k0 : 0;       // in the keys of the part
+    const uint32_t lane_t = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_t = lane_t + t * 128, o_t = lane_t + 256 + t * D;
+    float f0 = rsqrtf(static_cast<float>(D)) * 1.4426950408889634f, f1 = f0, factor = f0;
+    if (PAGED && n > 0) {
+      mbar_wait_warp(bar_q, 0, abort_flag, a.status);
+      factor = reinterpret_cast<const float*>(smem + SM::factor_off)[row];
+    }
+    float m = -INFINITY;
+    float2 l = make_float2(0.f, 0.f);
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      ok = ok && mbar_wait_warp(bar_s + 8 * t, j & 1, abort_flag, a.status);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t x[4][32];
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) tmem_ld32(s_t + q4 * 32, x[q4]);
+      if (PAGED) {
+        float2 ks;
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks.x), "=f"(ks.y) : "r"(sbase + SM::scale_off + (j & 7) * 8));
+        f0 = factor * ks.x;
+        f1 = a.PT == 64 ? factor * ks.y : f0;
+      }
+      tmem_wait_ld();
+      if (j >= it.whole_from[t]) {
+        const int valid = end - j * kKeys;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (q4 * 32 + e >= valid) x[q4][e] = 0xFF800000u;
+      }
+      float mx[4];
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        float v0 = fmax3(__uint_as_float(x[q4][0]), __uint_as_float(x[q4][1]), __uint_as_float(x[q4][2])), v1 = fmaxf(__uint_as_float(x[q4][3]), __uint_as_float(x[q4][4]));
+#pragma unroll
+        for (int e = 5; e < 29; e += 4) {
+          v0 = fmax3(v0, __uint_as_float(x[q4][e]), __uint_as_float(x[q4][e + 1]));
+          v1 = fmax3(v1, __uint_as_float(x[q4][e + 2]), __uint_as_float(x[q4][e + 3]));
+        }
+        mx[q4] = fmax3(fmax3(v0, __uint_as_float(x[q4][29]), __uint_as_float(x[q4][30])), v1, __uint_as_float(x[q4][31]));
+      }
+      const float top = PAGED ? fmaxf(fmaxf(mx[0], mx[1]) * f0, fmaxf(mx[2], mx[3]) * f1) : fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * f0;
+      const bool raise = top > m + kRaise;                         // (at first m is -inf)
+      if (__any_sync(0xffffffffu, raise)) {
+        const float to = raise ? top : m, alpha = raise ? (m == -INFINITY ? 0.f : fast_exp2(m - to)) : 1.f;
+        m = to;
+        l.x *= alpha;
+        l.y *= alpha;
+        if (j > 0) {
+          ok = mbar_wait_warp(bar_pv + 8 * t, (j - 1) & 1, abort_flag, a.status);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int q4 = 0; q4 < D / 16; ++q4) {
+            uint32_t v[16];
+            tmem_ld16(o_t + q4 * 16, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
+            tmem_st16(o_t + q4 * 16, v);
+          }
+        }
+      }
+      const float ref = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+      for (int q2 = 0; q2 < 2; ++q2) {
+        const float f = q2 ? f1 : f0;
+        const float2 ff = make_float2(f, f), rr = make_float2(ref, ref);
+        uint32_t p[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const uint32_t* v = &x[2 * q2 + (e >> 4)][2 * (e & 15)];
+          const float2 u = ffma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), ff, rr);
+          const float2 pr = make_float2(fast_exp2(u.x), fast_exp2(u.y));
+          p[e] = narrow2<M>(pr.x, pr.y);
+          if (kHalf) add_f16x2(l, p[e]);
+          else add_bf16x2(l, p[e]);
+        }
+        tmem_st32(s_t + q2 * 32, p);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive_warp(bar_p + 8 * t);
+    }
+    // ---- the row's end
+    if (ok && n > 0) ok = mbar_wait_warp(bar_pv + 8 * t, (n - 1) & 1, abort_flag, a.status);
+    tc_fence_after();
+    const float sum = l.x + l.y;
+    float unit = 1.f;
+    if (PAGED && n > 0) unit = fmaxf(fmaxf(unit_s[0], unit_s[1]), fmaxf(unit_s[2], unit_s[3]));
+    const int tok = s.t0 + i;
+    const int64_t part_row = (static_cast<int64_t>(it.part) * a.T + tok) * a.H + head;
+    const float inv = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
+    T* out = static_cast<T*>(a.out) + head * a.q_hs + tok * a.q_ts;
+    if (ok) {
+#pragma unroll 1
+      for (int q4 = 0; q4 < D / 32 && n > 0; ++q4) {
+        uint32_t v[32];
+        tmem_ld32(o_t + q4 * 32, v);
+        tmem_wait_ld();
+        if (!live) continue;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = sum == 0.f ? 0u : __float_as_uint(__uint_as_float(v[e]) * inv);
+        if (whole) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint4 o;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) (&o.x)[w] = narrow2<T>(__uint_as_float(v[8 * e + 2 * w]), __uint_as_float(v[8 * e + 2 * w + 1]));
+            *reinterpret_cast<uint4*>(out + q4 * 32 + 8 * e) = o;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(a.part_o + part_row * D + q4 * 32 + 4 * e) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+        }
+      }
+      if (!whole && live) a.part_ml[part_row] = make_float2(m, sum);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+  if (*spoilt_s && warp < kMoveWarp) {
+    const int last = min(it.rows, it.row0 + kRowsCta);
+    for (int r = it.row0 + warp; r < last; r += kMoveWarp) dense_row_whole<T, D, PAGED>(a, it.b, s.t0 + r / a.G, it.kvh * a.G + r % a.G, s, it.part);
+  }
+}
+
+int launch_dense_many(const DenseArgs& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int D, bool fp16, cudaStream_t st) {
+  // the sequences' last tiles are less than one each
+  const int64_t tiles = static_cast<int64_t>(a.T) * a.G / kRowsCta + (a.B < a.T ? a.B : a.T), ctas = tiles * a.KV;
+  if (ctas > INT32_MAX || a.parts > 65535) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  using Kern = void (*)(CUtensorMap, CUtensorMap, DenseArgs);
+  Kern kern;
+  if (a.kc) kern = fp16 ? (D == 128 ? many_kernel<__half, 128, true> : many_kernel<__half, 64, true>)
+                        : (D == 128 ? many_kernel<__nv_bfloat16, 128, true> : many_kernel<__nv_bfloat16, 64, true>);
+  else kern = fp16 ? (D == 128 ? many_kernel<__half, 128, false> : many_kernel<__half, 64, false>)
+                   : (D == 128 ? many_kernel<__nv_bfloat16, 128, false> : many_kernel<__nv_bfloat16, 64, false>);
+  const int smem = D == 128 ? ManySmem<128>::total : ManySmem<64>::total;
+  const int r = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
+  if (r != FASTAR_OK) return r;
+  return launch_chained(kern, dim3(static_cast<unsigned>(ctas), a.parts), kManyThreads, smem, st, tm_k, tm_v, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+}
+
+}  // namespace fastar

@@ -339,6 +339,22 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
       : "r"(taddr)
       : "memory");
 }
+// The same with 16 columns, load and store.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 // 16 lanes (from the address's lane on) x 64 consecutive columns, 16 x 256-bit fragments: r[4 i + 2 e + c] of thread t is lane
 // t / 4 + 8 e, column 8 i + 2 (t & 3) + c.
 __device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&r)[32]) {
@@ -439,6 +455,27 @@ __device__ __forceinline__ float2 fadd2(const float2& x, const float2& y) {
   float2 r;
   asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
   return r;
+}
+// 2^u of two logits on the FMA units, u < 2^22; 0 from -127 down, as the special-function units give it for a logit of -inf.  Adding 1.5 x 2^23
+// rounds u to the nearest integer, which goes to the exponent; 2^f of the rest, on [-1/2, 1/2], by a polynomial of degree 5 fitted to the least
+// relative error with 2^0 = 1.  Error 1.1e-7 at most, 1.7e-7 as worked out in fp32 (ex2.approx 1.2e-7); rounding to bf16 is 2e-3.
+__device__ __forceinline__ float2 poly_exp2(float2 u) {
+  auto both = [](float v) { return make_float2(v, v); };
+  constexpr float kRound = 12582912.f;                     // 1.5 x 2^23: the sum's last bits are the nearest integer
+  u.x = fmaxf(u.x, -127.f);
+  u.y = fmaxf(u.y, -127.f);
+  const float2 r = fadd2(u, both(kRound)), f = ffma2(fadd2(r, both(-kRound)), both(-1.f), u);
+  float2 y = both(0x1.5bba14p-10f);
+  y = ffma2(y, f, both(0x1.3cea88p-7f));
+  y = ffma2(y, f, both(0x1.c6b752p-5f));
+  y = ffma2(y, f, both(0x1.ebf9bcp-3f));
+  y = ffma2(y, f, both(0x1.62e42ap-1f));
+  y = ffma2(y, f, both(1.f));
+  return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(r.x) << 23)), __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(r.y) << 23)));
+}
+// Both halves of a bf16 pair to a sum each, as they are.
+__device__ __forceinline__ void add_bf16x2(float2& s, uint32_t b) {
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.bf16 %0, l, %0; add.f32.bf16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
 }
 // (x0, x1) *= f on accumulator bits
 __device__ __forceinline__ void scale2(uint32_t& x0, uint32_t& x1, const float2& f) {
