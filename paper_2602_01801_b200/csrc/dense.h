@@ -28,14 +28,20 @@ struct DenseArgs {
   const int32_t* table;            // [B][W]
   const int32_t* lens;             // [B]
   int W, pages, PT;
-  // keys in parts of `chunk`, whose results are joined by a kernel of their own (parts > 1)
+  int few_rows;                    // sequences of at most so many rows (tokens x G) belong to the kernel for few rows, the others to the one for many
+  // many rows: keys in parts of `chunk`, whose results are joined by a kernel of their own (parts > 1)
   int chunk, parts;
   float* part_o;                   // [parts][T][H][D]
   float2* part_ml;                 // [parts][T][H]  reference (binary orders) and sum
-  int few_rows;                    // sequences of at most so many rows (tokens x G) belong to the kernel for few rows, the others to the one for many
+  // few rows: items are cut where a CTA's share of all tiles ends (dense_few.cu)
+  int few_ctas;
+  float* few_o;                    // [2 few_ctas][few_rows][D]
+  float2* few_ml;                  // [2 few_ctas][few_rows]
+  int2* few_pieces;                // [T][H]  place of the row's first piece, and the last CTA that has one (-1: the row is not cut)
 };
 
 // A sequence: tokens [t0, t0 + n) of the packed axis, at positions [len - n, len) of its keys.
+constexpr int kFewKeys = 128;      // keys of a unit of the kernel for few rows
 struct DenseSeq {
   int t0, n, len;
 };
@@ -54,7 +60,7 @@ inline __host__ __device__ int check_seq(DenseSeq& s, int t0, int t1, int len, i
 // The keys that the token at position `pos` of a sequence of `len` sees: [0, end).
 inline __host__ __device__ int visible_end(int pos, int len, int frame) {
   if (frame == 0) return len;
-  const int64_t end = (static_cast<int64_t>(pos) / frame + 1) * frame;
+  const int64_t end = (static_cast<int64_t>(pos / frame) + 1) * frame;
   return end < len ? static_cast<int>(end) : len;
 }
 inline __host__ __device__ int pages_of(int tokens, int page_tokens) { return tokens / page_tokens + (tokens % page_tokens != 0 ? 1 : 0); }
@@ -95,6 +101,8 @@ struct AppendArgs {
 };
 int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st);
 int launch_dense_many(const DenseArgs& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int D, bool fp16, cudaStream_t st);
+int few_rows_of(int64_t rows);
+int few_ctas_an_sm(int rows, int D);
 int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 

@@ -65,38 +65,57 @@ int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int he
              : FASTAR_ERR_CUDA;
 }
 
-// How attention over the cache is launched: which kernels, and parts of how many keys (a multiple of 128).
+// How attention over the cache is launched: which kernels, on how many CTAs, the parts of the kernel for many rows (of a multiple of 128 keys), and the workspace.
 struct AttendPlan {
-  int few_rows;                    // 0: the kernel for few rows is not launched
-  bool many;
+  int few_rows, few_ctas;          // 0: the kernel for few rows is not launched
+  bool many, join;
   int chunk, parts;
+  size_t few_o, few_ml, few_pieces, part_o, part_ml, bytes;        // offsets
 };
-constexpr int kFewRows = 32;       // two tiles of rows read the keys twice, the second time out of L2
+constexpr int kFewRows = 32;
 constexpr int kSms = 148;
-AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV) {
+AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, int D) {
   AttendPlan p{};
   const int64_t G = H / KV, rows = static_cast<int64_t>(max_new) * G, len = max_len, tiles = (len + 127) / 128;
   p.many = rows > kFewRows;
   const bool equal = static_cast<int64_t>(B) * max_new <= T;       // the sequences may all be that long; if they are not, the kernel for many rows serves them too
-  p.few_rows = p.many && equal ? 0 : kFewRows;
-  int64_t parts = 1;
-  if (!p.many) {
-    // enough parts for four CTAs an SM, of 128 keys (a tile for each warp) at least
-    const int64_t units = static_cast<int64_t>(B) * ((rows + 15) / 16) * KV;
-    if (units < 4 * kSms) parts = 4 * kSms / units;
-    if (parts > tiles) parts = tiles;
-  } else {
+  p.chunk = static_cast<int>(tiles * 128);
+  p.parts = 1;
+  if (!p.many || !equal) {
+    // as many CTAs as the SMs hold, or one for every 128 keys where there are fewer of those
+    p.few_rows = few_rows_of(rows);
+    const int64_t units = static_cast<int64_t>(B) * KV * ((len + kFewKeys - 1) / kFewKeys), most = few_ctas_an_sm(p.few_rows, D) * kSms;
+    p.few_ctas = static_cast<int>(units < most ? units : most);
+    p.join = len > kFewKeys;
+  }
+  if (p.many) {
     // One CTA an SM: the parts that take the fewest rounds x (key tiles + 3, what a CTA takes to begin and end), with three more for the join
     const int64_t ctas = ((static_cast<int64_t>(T) * G + 255) / 256) * KV;
-    int64_t best = INT64_MAX;
+    int64_t best = INT64_MAX, parts = 1;
     for (int64_t k = 1; k <= 64 && k * 4 <= tiles + 3; ++k) {
       const int64_t cost = (ctas * k + kSms - 1) / kSms * ((tiles + k - 1) / k + 3) + (k > 1 ? 3 : 0);
       if (cost < best) { best = cost; parts = k; }
       if (ctas * k > 8 * kSms) break;
     }
+    p.chunk = static_cast<int>((tiles + parts - 1) / parts * 128);
+    p.parts = static_cast<int>((len + p.chunk - 1) / p.chunk);
+    p.join |= p.parts > 1;
   }
-  p.chunk = static_cast<int>(((len + parts - 1) / parts + 127) / 128 * 128);
-  p.parts = static_cast<int>((len + p.chunk - 1) / p.chunk);
+  auto take = [&](size_t bytes) {
+    const size_t at = p.bytes;
+    p.bytes += (bytes + 15) / 16 * 16;
+    return at;
+  };
+  p.bytes = 16;
+  if (p.few_ctas > 0) {
+    p.few_o = take(static_cast<size_t>(2 * p.few_ctas) * p.few_rows * D * 4);
+    p.few_ml = take(static_cast<size_t>(2 * p.few_ctas) * p.few_rows * 8);
+    p.few_pieces = take(static_cast<size_t>(T) * H * 8);
+  }
+  if (p.parts > 1) {
+    p.part_o = take(static_cast<size_t>(p.parts) * T * H * D * 4);
+    p.part_ml = take(static_cast<size_t>(p.parts) * T * H * 8);
+  }
   return p;
 }
 }  // namespace
@@ -149,10 +168,7 @@ extern "C" size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t
   if (shape_ok(num_heads, num_kv_heads, head_dim, FASTAR_BF16) != FASTAR_OK || num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new ||
       too_long(total_tokens, max_len, num_heads, num_kv_heads))
     return 0;
-  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads);
-  if (p.parts == 1) return 16;
-  const size_t rows = static_cast<size_t>(p.parts) * total_tokens * num_heads;
-  return rows * (head_dim + 2) * 4 + 16;
+  return attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim).bytes;
 }
 
 extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_stride, int64_t token_stride, const uint8_t* k_codes, const uint8_t* v_codes,
@@ -180,17 +196,19 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   a.cu = cu; a.frame = frame_len; a.max_new = max_new; a.max_len = max_len;
   a.kc = k_codes; a.vc = v_codes; a.ks = k_scale; a.vs = v_scale; a.table = table; a.lens = lens;
   a.W = table_width; a.pages = num_pages; a.PT = page_tokens;
-  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads);
-  a.parts = p.parts; a.chunk = p.chunk; a.few_rows = p.few_rows;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<size_t>(p.parts) * total_tokens * num_heads * head_dim);
+  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim);
+  uint8_t* w = static_cast<uint8_t*>(workspace);
+  a.few_rows = p.few_rows; a.few_ctas = p.few_ctas;
+  a.few_o = reinterpret_cast<float*>(w + p.few_o); a.few_ml = reinterpret_cast<float2*>(w + p.few_ml); a.few_pieces = reinterpret_cast<int2*>(w + p.few_pieces);
+  a.parts = p.parts; a.chunk = p.chunk;
+  a.part_o = reinterpret_cast<float*>(w + p.part_o); a.part_ml = reinterpret_cast<float2*>(w + p.part_ml);
   r = dense_device(&a.status);
   if (r != FASTAR_OK) return r;
   const bool fp16 = dtype == FASTAR_FP16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (p.few_rows > 0) r = launch_dense_few(a, head_dim, fp16, st);
+  if (p.few_ctas > 0) r = launch_dense_few(a, head_dim, fp16, st);
   if (r == FASTAR_OK && p.many) r = launch_dense_many(a, CUtensorMap{}, CUtensorMap{}, head_dim, fp16, st);
-  if (r == FASTAR_OK && p.parts > 1) r = launch_dense_join(a, head_dim, fp16, st);
+  if (r == FASTAR_OK && p.join) r = launch_dense_join(a, head_dim, fp16, st);
   return r;
 }
 

@@ -1,14 +1,15 @@
 // Attention over the 8-bit cache for sequences with few rows (new tokens x query heads of a key head), one token above all, and the join of parts.
 //
-//   x_rj = q_r . (c_j s_page) / sqrt(d),   p = exp2(x - m),   o_r = sum_j p_rj (w_j u_page) / sum_j p_rj     (codes c, w; scales s, u)
+//   x_jr = (c_j s_page) . q_r / sqrt(d),   p = exp2(x - m),   o_r = sum_j p_jr (w_j u_page) / sum_j p_jr     (codes c, w; scales s, u)
 //
-// Every code is read once and used for a few rows only, so memory bounds it: 2 d bytes a key and head.  A CTA takes a part of the keys of one (sequence, key
-// head, 16 rows); its four warps take tiles of 32 keys in turn, each with a ring and a soft-max of its own, so that nobody waits for anybody until the end, where
-// the four are added up in shared memory.  Rows whose keys are cut into parts go through memory and are joined by a kernel of their own (join_kernel).
-//   - The products are m16n8k16 with fp16 operands: e4m3 values are fp16 values, and one instruction converts two.  Queries are divided by a power of two so that
-//     the row's largest is in [1, 2): fp16 then holds them to 2^-25 of it, better than their own type.  Probabilities are at most 1.
+// Every code is read once and used for a few rows only, so memory bounds it: 2 d bytes a key and head.  The four warps of a CTA take tiles of keys in turn, each with
+// a ring and a soft-max of its own, so that nobody waits for anybody until the end of a piece, where the four are added up in shared memory.
+//   - Keys are the products' rows (m16n8k16: 16 keys x 8 query rows), so one token's few rows fill an instruction, and 8, 16 or 32 rows share a key's conversion.
+//   - fp16 operands: e4m3 values are fp16 values, and one instruction converts two.  Queries are divided by a power of two so that the row's largest is in [1, 2):
+//     fp16 then holds them to 2^-25 of it, better than their own type.  Probabilities are 2^8 at most.
 //   - The order of the d products of a logit is free, so a thread takes 32 neighbouring codes of a key (two 16-byte reads) as its part of eight k-steps.
-//   - Values come through ldmatrix.trans as pairs of neighbouring columns; even and odd columns are separate n-tiles, so one byte permutation makes both operands.
+//   - Values come through ldmatrix.trans as pairs of neighbouring columns; even and odd columns are rows 0-7 and 8-15 of the product's first operand, so one byte
+//     permutation makes two operands.  Probabilities turn by movmatrix.
 //   - A page's value scale is a unit of the accumulators: they are multiplied by a power of two where it changes from page to page, exactly.  The unit is kept
 //     within 2^60 of the largest seen, so that a page of zeros (scale 2^-126) does not take the sums out of range.
 //   - The row sums add up the probabilities as rounded.
@@ -18,17 +19,22 @@
 
 namespace fastar {
 
-constexpr int kFewThreads = 128, kFewTile = 32, kFewStages = 3;
+constexpr int kFewThreads = 128;
+constexpr float kFewRaise = 8.f;                                   // the reference is raised when a logit exceeds it by so many binary orders
+constexpr float kLeastScale = 1.17549435e-38f, kUnitSpan = 8.67361738e-19f;      // 2^-126, 2^-60
 
-template <int D>
-struct FewSmem {
-  static constexpr int tile = kFewTile * D;                        // bytes of a tile of keys, or of values
+// NR: groups of 8 rows; TILE keys of a warp's tile, in STAGES stages
+template <int D, int NR>
+struct FewConf {
+  // Tiles of 16 keys leave room for four CTAs an SM where there are 8 rows; with more rows they do not, and 32 keys a tile are better
+  static constexpr int TILE = NR == 1 ? 16 : 32, STAGES = 2, CTAS = NR == 1 ? 4 : 2;
+  static constexpr int tile = TILE * D;                            // bytes of a tile of keys, or of values
   static constexpr int stage = 2 * tile;
-  static constexpr int scales = 4 * kFewStages * stage;            // [4][stages][2] floats behind the rings
-  static constexpr int total = scales + 4 * kFewStages * 8;
+  static constexpr int scales = 4 * STAGES * stage;                // [4][stages][2] floats behind the rings
   static constexpr int pitch = D + 4;                              // floats of a row in the join of the warps
-  static constexpr int stat = 4 * 16 * pitch * 4;                  // [4][16] (m, l) behind the rows
-  static_assert(stat + 4 * 16 * 8 <= scales, "the join takes the rings' place");
+  static constexpr int join = scales + 4 * STAGES * 8;
+  static constexpr int stat = join + 4 * 8 * NR * pitch * 4;       // [4][8 NR] (m, l) behind the rows
+  static constexpr int total = stat + 4 * 8 * NR * 8;
 };
 
 // Where a 16-byte piece of a row lies: eight rows' same piece, and a row pair's neighbouring ones, fall into different banks.
@@ -49,6 +55,14 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&v)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at));
 }
+__device__ __forceinline__ uint32_t turn8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
 }
@@ -60,247 +74,410 @@ __device__ __forceinline__ uint32_t without_nan_codes(uint32_t v, bool& any) {
   return v & ~nan;
 }
 
-template <class T, int D>
-__global__ void __launch_bounds__(kFewThreads) few_kernel(const DenseArgs a, int row_tiles) {
-  using SM = FewSmem<D>;
+// The units (128 keys of a key head) of a sequence, sequences after one another, in a sequence key heads after one another.  CTA c of n takes the units
+// [U c / n, U (c + 1) / n): all have the same share, whatever the lengths are, and a CTA has two cut items at most, its first and its last.
+struct FewSeq {
+  DenseSeq s;
+  int tiles;                                                       // of 128 keys
+  int64_t units;
+};
+__device__ __forceinline__ int64_t few_seq(const DenseArgs& a, int b, FewSeq& f) {
+  const int r = seq_of(a, b, f.s);
+  if (r < 0 && a.status) record_status(a.status, kErrBounds);
+  f.tiles = f.s.n * a.G <= a.few_rows ? f.s.len / kFewKeys + (f.s.len % kFewKeys != 0 ? 1 : 0) : 0;
+  return f.units = static_cast<int64_t>(f.tiles) * a.KV;
+}
+// A CTA's way through its pieces.
+struct FewWalk {
+  int b;
+  FewSeq f;
+  int64_t base, x, x_end;                                          // units before the sequence; the next piece's first; the CTA's end
+  // the piece: key head, tiles [tile0, tile1) of the item, keys [k0, k1) of which some row sees all
+  int kvh, tile0, tile1, k0, k1;
+  __device__ __forceinline__ bool next(const DenseArgs& a) {
+    if (x >= x_end) return false;
+    if (x - base == f.units) {                                     // the next sequence that has some
+      base += f.units;
+      while (few_seq(a, ++b, f) == 0) {}
+    }
+    const int64_t at = x - base;
+    kvh = f.units <= INT32_MAX ? static_cast<int>(at) / f.tiles : static_cast<int>(at / f.tiles);
+    tile0 = static_cast<int>(at - static_cast<int64_t>(kvh) * f.tiles);
+    tile1 = static_cast<int>(min(static_cast<int64_t>(f.tiles), tile0 + x_end - x));
+    x += tile1 - tile0;
+    k0 = tile0 * kFewKeys;
+    k1 = min(visible_end(f.s.len - 1, f.s.len, a.frame), tile1 == f.tiles ? f.s.len : tile1 * kFewKeys);
+    return true;
+  }
+};
+__device__ __forceinline__ int64_t few_first(int64_t units, int c, int n) { return units * c / n; }
+__device__ __forceinline__ int few_cta_of(int64_t units, int64_t x, int n) { return static_cast<int>(((x + 1) * n - 1) / units); }
+
+template <class T, int D, int NR>
+__global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(const DenseArgs a) {
+  using SM = FewConf<D, NR>;
+  constexpr int TILE = SM::TILE, STAGES = SM::STAGES, MT = TILE / 16, R = 8 * NR;
   constexpr int KS = D / 16;                                       // k-steps of a logit, and 16-column blocks of the values
   extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int64_t found_s[3];                                   // all units, those before the sequence that this CTA begins in, that sequence
   const uint32_t sbase = smem_u32(smem);
   const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const int b = blockIdx.x / row_tiles, rt = blockIdx.x % row_tiles, part = blockIdx.y, kvh = blockIdx.z;
   chain_wait();
-  DenseSeq s;
-  const int found = seq_of(a, b, s);
-  if (found < 0 && threadIdx.x == 0 && a.status) record_status(a.status, kErrBounds);
-  if (found <= 0) return;
-  const int rows = s.n * a.G;
-  if (rows > a.few_rows || rt * 16 >= rows) return;
-  const bool whole = a.parts == 1 || s.len <= a.chunk;
-  if (whole ? part > 0 : static_cast<int64_t>(part) * a.chunk >= s.len) return;
-  const int past = s.len - s.n, r_last = min(rows, rt * 16 + 16) - 1;
-  const int see_all = visible_end(past + rt * 16 / a.G, s.len, a.frame), see_any = visible_end(past + r_last / a.G, s.len, a.frame);
-  const int k0 = whole ? 0 : part * a.chunk, k1 = whole ? see_any : min(see_any, k0 + a.chunk);
-
-  // this thread's rows: their end, their queries as fp16 operands and what those were divided by
-  int end[2];
-  float factor[2];
-  uint32_t qf[KS][4];
+  chain_next();
+  {
+    int64_t* red = reinterpret_cast<int64_t*>(smem);
+    FewSeq f;
+    auto scan = [&](int b, int64_t& mine, int64_t& step) {         // units before sequence b of this step's, b's and the step's
+      mine = b < a.B ? few_seq(a, b, f) : 0;
+      int64_t x = mine;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = rt * 16 + g + 8 * h;
-    const bool live = r < rows;
-    const int i = live ? r / a.G : 0, head = kvh * a.G + (live ? r % a.G : 0);
-    end[h] = live ? visible_end(past + i, s.len, a.frame) : 0;
-    const T* src = static_cast<const T*>(a.q) + head * a.q_hs + (s.t0 + i) * a.q_ts + c * (D / 4);
-    uint4 v[D / 32];
-    uint32_t most = 0;
-#pragma unroll
-    for (int w = 0; w < D / 32; ++w) {
-      v[w] = live ? *reinterpret_cast<const uint4*>(src + 8 * w) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = widen2<T>((&v[w].x)[e]);
-        most = max(most, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+      for (int w = 1; w < 32; w <<= 1) {
+        const int64_t u = __shfl_up_sync(0xffffffffu, x, w);
+        if (lane >= w) x += u;
       }
+      __syncthreads();
+      if (lane == 31) red[warp] = x;
+      __syncthreads();
+      int64_t off = 0;
+      step = 0;
+#pragma unroll
+      for (int w = 0; w < kFewThreads / 32; ++w) {
+        if (w < warp) off += red[w];
+        step += red[w];
+      }
+      return off + x - mine;
+    };
+    int64_t mine, step, before = scan(threadIdx.x, mine, step), all = step;
+    for (int b0 = kFewThreads; b0 < a.B; b0 += kFewThreads) {
+      int64_t unused;
+      scan(b0 + threadIdx.x, unused, step);
+      all += step;
     }
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    int e = static_cast<int>(most >> 23) - 127;
-    e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));        // (a row that is not finite stays as it is)
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    factor[h] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (rsqrtf(static_cast<float>(D)) * 1.4426950408889634f);
-#pragma unroll
-    for (int w = 0; w < D / 32; ++w)
-#pragma unroll
-      for (int e2 = 0; e2 < 4; ++e2) {
-        const float2 f = widen2<T>((&v[w].x)[e2]);
-        qf[2 * w + (e2 >> 1)][h + 2 * (e2 & 1)] = f16x2_of(f.x * down, f.y * down);
+    const int n = all < gridDim.x ? static_cast<int>(all) : gridDim.x;
+    if (static_cast<int>(blockIdx.x) >= n) return;
+    const int64_t first = few_first(all, blockIdx.x, n);
+    int64_t base = 0;
+    for (int b0 = 0;; b0 += kFewThreads) {                         // (the first step's sums are at hand)
+      if (b0 > 0 || a.B > kFewThreads) before = scan(b0 + threadIdx.x, mine, step);
+      else step = all;
+      if (mine > 0 && first >= base + before && first < base + before + mine) {
+        found_s[0] = all;
+        found_s[1] = base + before;
+        found_s[2] = b0 + threadIdx.x;
       }
+      base += step;
+      if (base > first) break;
+    }
+    __syncthreads();
   }
+  const int64_t units = found_s[0];
+  const int ctas = units < gridDim.x ? static_cast<int>(units) : gridDim.x;
+  FewWalk walk, asked;
+  walk.b = static_cast<int>(found_s[2]);
+  walk.base = found_s[1];
+  walk.x = few_first(units, blockIdx.x, ctas);
+  walk.x_end = few_first(units, blockIdx.x + 1, ctas);
+  few_seq(a, walk.b, walk.f);
+  asked = walk;
 
-  const uint32_t ring = sbase + warp * kFewStages * SM::stage, scale_s = sbase + SM::scales + warp * kFewStages * 8;
-  // pages of the sequence, 32 at a time, one a lane
-  const int n_pages = pages_of(s.len, a.PT);
-  int window = -64, window_page = 0;
-  const int tiles = k1 > k0 ? (k1 - k0 + kFewTile - 1) / kFewTile : 0;
-  auto ask = [&](int t) {                                          // tile t goes into its stage; an empty group past the end
-    if (t < tiles) {
-      const int key0 = k0 + t * kFewTile, p = key0 / a.PT;
-      if (p - window >= 32 || window < 0) {
+  // ---- copies: a warp's tiles of all pieces, one after the other
+  const uint32_t ring = sbase + warp * STAGES * SM::stage, scale_s = sbase + SM::scales + warp * STAGES * 8;
+  constexpr int PPR = D / 16, RPI = 32 / PPR, COPIES = TILE / RPI;             // 16-byte pieces a row, rows an instruction, instructions a tile
+  const int my_row = lane / PPR, my_piece = lane % PPR;
+  uint32_t ask_st = 0;
+  int key0_ask = 0, window = 0, window_page = 0;                   // pages of the sequence, 32 at a time, one a lane
+  asked.k1 = 0;
+  bool more = true;
+  auto ask = [&]() {                                               // the next tile goes into its stage; an empty group past the end
+    while (more && key0_ask >= asked.k1) {
+      more = asked.next(a);
+      key0_ask = asked.k0 + warp * TILE;
+      window = -64;
+    }
+    if (more) {
+      const int p = key0_ask / a.PT;
+      if (p - window >= 32) {
         window = p;
-        window_page = p + lane < n_pages ? page_of(a, b, p + lane) : 0;
+        window_page = p + lane < pages_of(asked.f.s.len, a.PT) ? page_of(a, asked.b, p + lane) : 0;
       }
-      const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p - window)) * a.KV + kvh;
-      const int64_t off = (at * a.PT + key0 % a.PT) * D;
-      const int st = (t / 4) % kFewStages;
-      const uint32_t dst = ring + st * SM::stage;
-      constexpr int PPR = D / 16, RPI = 32 / PPR;                  // pieces a row, rows an instruction
-      const int piece = lane % PPR;
+      const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p - window)) * a.KV + asked.kvh;
+      const int64_t off = (at * a.PT + key0_ask % a.PT) * D;
+      const uint32_t dst = ring + ask_st * SM::stage;
+      const int rows_there = asked.k1 - key0_ask;
+      if (rows_there >= TILE) {
+        const uint8_t *k_src = a.kc + off + lane * 16, *v_src = a.vc + off + lane * 16;
 #pragma unroll
-      for (int i = 0; i < kFewTile / RPI; ++i) {
-        const int row = i * RPI + lane / PPR;
-        const bool there = key0 + row < k1;
-        const int64_t from = off + (there ? row * D + piece * 16 : 0);
-        cp_async16(dst + few_at<D>(row, piece), a.kc + from, there);
-        cp_async16(dst + SM::tile + few_at<D>(row, piece), a.vc + from, there);
+        for (int i = 0; i < COPIES; ++i) {
+          const uint32_t to = dst + i * 512 + few_at<D>(my_row + (i & 1) * RPI, my_piece) - (i & 1) * 512;
+          cp_async16(to, k_src + i * 512);
+          cp_async16(to + SM::tile, v_src + i * 512);
+        }
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < COPIES; ++i) {
+          const int row = i * RPI + my_row;
+          const bool there = row < rows_there;
+          const int64_t from = off + (there ? row * D + my_piece * 16 : 0);
+          cp_async16(dst + few_at<D>(row, my_piece), a.kc + from, there);
+          cp_async16(dst + SM::tile + few_at<D>(row, my_piece), a.vc + from, there);
+        }
       }
-      if (lane < 2) cp_async4(scale_s + st * 8 + lane * 4, (lane ? a.vs : a.ks) + at);
+      if (lane < 2) cp_async4(scale_s + ask_st * 8 + lane * 4, (lane ? a.vs : a.ks) + at);
+      key0_ask += 4 * TILE;
+      ask_st = ask_st + 1 == STAGES ? 0 : ask_st + 1;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) ask();
+  uint32_t st = 0;
 
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[KS][2][4];
-#pragma unroll
-  for (int k = 0; k < KS; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[k][0][e] = o[k][1][e] = 0.f;
-  float unit = 1.17549435e-38f, most_unit = 0.f;
-  bool spoilt = false;
-#pragma unroll
-  for (int i = 0; i < kFewStages - 1; ++i) ask(warp + 4 * i);
-  for (int t = warp; t < tiles; t += 4) {
-    ask(t + 4 * (kFewStages - 1));
-    asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 1) : "memory");
-    __syncwarp();
-    const int st = (t / 4) % kFewStages;
-    const uint32_t ks_s = ring + st * SM::stage, vs_s = ks_s + SM::tile;
-    float k_scale, v_scale;
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(k_scale), "=f"(v_scale) : "r"(scale_s + st * 8));
-    // logits
-    float x[4][4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
-      uint32_t w[D / 16];
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        const uint4 v = lds128(ks_s + few_at<D>(n * 8 + g, c * (D / 64) + i));
-        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-      }
-#pragma unroll
-      for (int k = 0; k < KS; ++k) mma_f16(x[n], qf[k], e4m3x2_to_half2(w[k] & 0xFFFFu), e4m3x2_to_half2(w[k] >> 16));
+  for (bool first_piece = true; walk.next(a); first_piece = false) {
+    const DenseSeq s = walk.f.s;
+    const int b = walk.b, kvh = walk.kvh, k0 = walk.k0, k1 = walk.k1;
+    const bool whole = walk.tile0 == 0 && walk.tile1 == walk.f.tiles;
+    const int place = (2 * blockIdx.x + (first_piece ? 0 : 1)) * R;            // where a cut item's piece goes
+    const int rows = s.n * a.G, past = s.len - s.n;
+    const int see_all = visible_end(past, s.len, a.frame);
+    if (walk.tile0 == 0 && static_cast<int>(threadIdx.x) < rows) {
+      const int r = threadIdx.x, last = whole ? -1 : few_cta_of(units, walk.x - walk.tile1 + walk.f.tiles - 1, ctas);      // the CTA that has the item's last unit
+      a.few_pieces[static_cast<int64_t>(s.t0 + r / a.G) * a.H + kvh * a.G + r % a.G] = make_int2(place / R, last);
     }
-    const int key0 = k0 + t * kFewTile;
-    const bool masked = key0 + kFewTile > see_all;
-    const float f0 = factor[0] * k_scale, f1 = factor[1] * k_scale;
-    float mx[2] = {-INFINITY, -INFINITY};
+
+    // queries: row g of every group, this thread's D / 4 columns, as fp16 operands; what they were divided by goes to those who have the row's logits
+    uint32_t qf[NR][KS][2];
+    float factor[NR][2];
+    int end[NR][2];
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int n = 0; n < NR; ++n) {
+      const int r = n * 8 + g;
+      const bool live = r < rows;
+      const int i = live ? r / a.G : 0, head = kvh * a.G + (live ? r - i * a.G : 0);
+      const T* src = static_cast<const T*>(a.q) + head * a.q_hs + (s.t0 + i) * a.q_ts + c * (D / 4);
+      uint4 v[D / 32];
+      uint32_t most = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float& v = x[n][e];
-        v *= e < 2 ? f0 : f1;
-        if (masked && key0 + n * 8 + 2 * c + (e & 1) >= end[e >> 1]) v = -INFINITY;
-        mx[e >> 1] = fmaxf(mx[e >> 1], v);
+      for (int w = 0; w < D / 32; ++w) {
+        v[w] = live ? *reinterpret_cast<const uint4*>(src + 8 * w) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = widen2<T>((&v[w].x)[e]);
+          most = max(most, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+        }
       }
-    // the accumulators' unit
-    most_unit = fmaxf(most_unit, v_scale);
-    const float to = fmaxf(fmaxf(v_scale, most_unit * 8.67361738e-19f), 1.17549435e-38f), p_factor = v_scale / to;
-    float alpha[2], ref[2];
-    const float change = unit / to;
-    unit = to;
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      int e = static_cast<int>(most >> 23) - 127;
+      e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));      // (a row that is not finite stays as it is)
+      const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (rsqrtf(static_cast<float>(D)) * 1.4426950408889634f);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-      mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
-      const float top = fmaxf(m[h], mx[h]);
-      alpha[h] = m[h] == -INFINITY ? 0.f : fast_exp2(m[h] - top);
-      m[h] = top;
-      ref[h] = top == -INFINITY ? 0.f : top;
-      l[h] *= alpha[h];
-      alpha[h] *= change;
+      for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+        for (int e2 = 0; e2 < 4; ++e2) {
+          const float2 f = widen2<T>((&v[w].x)[e2]);
+          qf[n][2 * w + (e2 >> 1)][e2 & 1] = f16x2_of(f.x * down, f.y * down);
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        factor[n][h] = __shfl_sync(0xffffffffu, up, (2 * c + h) * 4);
+        const int r2 = n * 8 + 2 * c + h;
+        end[n][h] = r2 < rows ? visible_end(past + r2 / a.G, s.len, a.frame) : 0;
+      }
     }
-    if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+
+    float m[NR][2], o[KS][NR][4];
+    float2 l[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n] = make_float2(0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[k][0][e] *= alpha[e >> 1];
-          o[k][1][e] *= alpha[e >> 1];
+        for (int e = 0; e < 4; ++e) o[k][n][e] = 0.f;
+    }
+    float unit = kLeastScale, most_unit = 0.f;
+    bool spoilt = false;
+    auto tile = [&](int key0, auto way) {
+      constexpr bool MASKED = decltype(way)::value;
+      const uint32_t ks_s = ring + st * SM::stage, vs_s = ks_s + SM::tile;
+      float k_scale, v_scale;
+      asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(k_scale), "=f"(v_scale) : "r"(scale_s + st * 8));
+      // logits: x[mt][n][e] is key mt 16 + g + 8 (e / 2), row n 8 + 2 c + e % 2
+      float x[MT][NR][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) x[mt][n][0] = x[mt][n][1] = x[mt][n][2] = x[mt][n][3] = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const uint4 v0 = lds128(ks_s + few_at<D>(mt * 16 + g, c * (D / 64) + i)), v1 = lds128(ks_s + few_at<D>(mt * 16 + g + 8, c * (D / 64) + i));
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t k[4];
+            e4m3x4_to_half2((&v0.x)[w], k[0], k[2]);
+            e4m3x4_to_half2((&v1.x)[w], k[1], k[3]);
+#pragma unroll
+            for (int n = 0; n < NR; ++n) mma_f16(x[mt][n], k, qf[n][4 * i + w][0], qf[n][4 * i + w][1]);
+          }
         }
+      }
+      if (MASKED) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (key0 + mt * 16 + g + 8 * (e >> 1) >= end[n][e & 1]) x[mt][n][e] = -INFINITY;
+      }
+      // the reference is raised for all rows of the warp at once; the accumulators follow it, and their unit
+      most_unit = fmaxf(most_unit, v_scale);
+      const float to = fmaxf(fmaxf(v_scale, most_unit * kUnitSpan), kLeastScale);
+      float mx[NR][2];
+      bool change = to != unit;
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v = fmaxf(x[0][n][h], x[0][n][2 + h]);
+#pragma unroll
+          for (int mt = 1; mt < MT; ++mt) v = fmax3(v, x[mt][n][h], x[mt][n][2 + h]);
+          mx[n][h] = v * (factor[n][h] * k_scale);
+          change |= mx[n][h] > m[n][h] + kFewRaise;
+        }
+      if (__any_sync(0xffffffffu, change)) {
+        const float ratio = unit / to;
+        unit = to;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          float alpha[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) mx[n][h] = fmaxf(mx[n][h], __shfl_xor_sync(0xffffffffu, mx[n][h], w));
+            const float top = fmaxf(m[n][h], mx[n][h]);
+            alpha[h] = m[n][h] == -INFINITY ? 0.f : fast_exp2(m[n][h] - top);
+            m[n][h] = top;
+          }
+          l[n].x *= alpha[0];
+          l[n].y *= alpha[1];
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[k][n][e] *= alpha[e & 1] * ratio;
+        }
+      }
+      const float p_factor = v_scale / unit;
+      uint32_t p[MT][NR][2];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const float2 f = make_float2(factor[n][0] * k_scale, factor[n][1] * k_scale);
+        const float2 ref = make_float2(m[n][0] == -INFINITY ? 0.f : -m[n][0], m[n][1] == -INFINITY ? 0.f : -m[n][1]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 u = ffma2(make_float2(x[mt][n][2 * h], x[mt][n][2 * h + 1]), f, ref);
+            uint32_t v = f16x2_of(fast_exp2(u.x), fast_exp2(u.y));
+            add_f16x2(l[n], v);
+            if (p_factor != 1.f) {                                 // (a page whose scale is below 2^-60 of the largest)
+              const float2 r = __half22float2(*reinterpret_cast<__half2*>(&v));
+              v = f16x2_of(r.x * p_factor, r.y * p_factor);
+            }
+            p[mt][n][h] = turn8x8(v);
+          }
+      }
+      // o[k][n][e] is column 16 k + 2 g + e / 2, row n 8 + 2 c + e % 2
+#pragma unroll
+      for (int k = 0; k < KS; k += 2 / MT) {
+        uint32_t v[4];
+        // four 8 x 8 blocks: 32 keys of one block of columns, or 16 keys of two
+        ldmatrix4_trans(v, vs_s + (MT == 2 ? few_at<D>(lane, k) : few_at<D>(lane & 15, k + (lane >> 4))));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t u = v[2 * i + h];
+            if (MASKED) u = without_nan_codes(u, spoilt);
+            e4m3x4_to_half2(__byte_perm(u, 0u, 0x3120), w[2 * h], w[2 * h + 1]);
+          }
+          const int kk = MT == 2 ? k : k + i, mt = MT == 2 ? i : 0;
+#pragma unroll
+          for (int n = 0; n < NR; ++n) mma_f16(o[kk][n], w, p[mt][n][0], p[mt][n][1]);
+        }
+      }
+      st = st + 1 == STAGES ? 0 : st + 1;
+    };
+    for (int key0 = k0 + warp * TILE; key0 < k1; key0 += 4 * TILE) {
+      ask();
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      __syncwarp();
+      if (key0 + TILE <= see_all) tile(key0, std::false_type{});
+      else tile(key0, std::true_type{});
+      __syncwarp();                                                // the stage may be filled again
     }
-    uint32_t p[2][4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float p0 = fast_exp2(x[n][2 * h] - ref[h]), p1 = fast_exp2(x[n][2 * h + 1] - ref[h]);
-        uint32_t v = f16x2_of(p0, p1);
-        const float2 r = __half22float2(*reinterpret_cast<__half2*>(&v));
-        l[h] += r.x + r.y;
-        if (p_factor != 1.f) v = f16x2_of(r.x * p_factor, r.y * p_factor);
-        p[n >> 1][h + 2 * (n & 1)] = v;
-      }
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      uint32_t v[4];
-      ldmatrix4_trans(v, vs_s + few_at<D>(lane, k));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (masked) v[i] = without_nan_codes(v[i], spoilt);
-        v[i] = __byte_perm(v[i], 0u, 0x3120);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        mma_f16(o[k][0], p[h], e4m3x2_to_half2(v[2 * h] & 0xFFFFu), e4m3x2_to_half2(v[2 * h + 1] & 0xFFFFu));
-        mma_f16(o[k][1], p[h], e4m3x2_to_half2(v[2 * h] >> 16), e4m3x2_to_half2(v[2 * h + 1] >> 16));
-      }
-    }
-    __syncwarp();                                                  // the stage may be filled again
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
 
-  if (__syncthreads_or(spoilt ? 1 : 0)) {
-    // values that are no numbers where some row does not see them: straight from the definition
-    for (int r = rt * 16 + warp; r <= r_last; r += 4) dense_row_whole<T, D, true>(a, b, s.t0 + r / a.G, kvh * a.G + r % a.G, s, part);
-    return;
-  }
-  // the warps' rows, with their units
-  float* join = reinterpret_cast<float*>(smem);
-  float2* stat = reinterpret_cast<float2*>(smem + SM::stat);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-    const int row = warp * 16 + g + 8 * h;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-      *reinterpret_cast<float4*>(join + row * SM::pitch + 16 * k + 4 * c) =
-          make_float4(o[k][0][2 * h] * unit, o[k][1][2 * h] * unit, o[k][0][2 * h + 1] * unit, o[k][1][2 * h + 1] * unit);
-    if (c == 0) stat[row] = make_float2(m[h], l[h]);
-  }
-  __syncthreads();
-  const int row = threadIdx.x >> 3, r = rt * 16 + row;
-  if (r >= rows) return;
-  float top = -INFINITY, sum = 0.f, f[4];
-#pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[w * 16 + row].x);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float2 ml = stat[w * 16 + row];
-    f[w] = ml.x == -INFINITY && ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
-    sum = fmaf(ml.y, f[w], sum);
-  }
-  const int t = s.t0 + r / a.G, head = kvh * a.G + r % a.G;
-  const int64_t part_row = (static_cast<int64_t>(part) * a.T + t) * a.H + head;
-  const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
-  T* out = static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    const int col = 32 * i + 4 * (threadIdx.x & 7);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float4 x = *reinterpret_cast<const float4*>(join + (w * 16 + row) * SM::pitch + col);
-      v.x = fmaf(x.x, f[w], v.x);
-      v.y = fmaf(x.y, f[w], v.y);
-      v.z = fmaf(x.z, f[w], v.z);
-      v.w = fmaf(x.w, f[w], v.w);
+    if (__syncthreads_or(spoilt ? 1 : 0)) {
+      // values that are no numbers where some row does not see them: straight from the definition
+      for (int r = warp; r < rows; r += 4)
+        dense_row_to<T, D, true>(a, b, s.t0 + r / a.G, kvh * a.G + r % a.G, s, k0, k1, whole, a.few_o + static_cast<int64_t>(place + r) * D, a.few_ml + place + r);
+      continue;
     }
-    if (whole) *reinterpret_cast<uint2*>(out + col) = make_uint2(narrow2<T>(v.x * inv, v.y * inv), narrow2<T>(v.z * inv, v.w * inv));
-    else *reinterpret_cast<float4*>(a.part_o + part_row * D + col) = v;
+    // the warps' rows, with their units
+    float* join = reinterpret_cast<float*>(smem + SM::join);
+    float2* stat = reinterpret_cast<float2*>(smem + SM::stat);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) {
+        l[n].x += __shfl_xor_sync(0xffffffffu, l[n].x, w);
+        l[n].y += __shfl_xor_sync(0xffffffffu, l[n].y, w);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = warp * R + n * 8 + 2 * c + h;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) *reinterpret_cast<float2*>(join + row * SM::pitch + 16 * k + 2 * g) = make_float2(o[k][n][h] * unit, o[k][n][2 + h] * unit);
+        if (g == 0) stat[row] = make_float2(m[n][h], h ? l[n].y : l[n].x);
+      }
+    }
+    __syncthreads();
+    constexpr int TPW = kFewThreads / R;                           // threads a row
+    const int r = threadIdx.x / TPW;
+    if (r < rows) {
+      float top = -INFINITY, sum = 0.f, f[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[w * R + r].x);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2 ml = stat[w * R + r];
+        f[w] = ml.x == -INFINITY && ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
+        sum = fmaf(ml.y, f[w], sum);
+      }
+      const int t = s.t0 + r / a.G, head = kvh * a.G + r % a.G;
+      const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+      T* out = static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts;
+#pragma unroll
+      for (int i = 0; i < D / (4 * TPW); ++i) {
+        const int col = 4 * TPW * i + 4 * (threadIdx.x % TPW);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float4 x4 = *reinterpret_cast<const float4*>(join + (w * R + r) * SM::pitch + col);
+          v.x = fmaf(x4.x, f[w], v.x);
+          v.y = fmaf(x4.y, f[w], v.y);
+          v.z = fmaf(x4.z, f[w], v.z);
+          v.w = fmaf(x4.w, f[w], v.w);
+        }
+        if (whole) *reinterpret_cast<uint2*>(out + col) = make_uint2(narrow2<T>(v.x * inv, v.y * inv), narrow2<T>(v.z * inv, v.w * inv));
+        else *reinterpret_cast<float4*>(a.few_o + static_cast<int64_t>(place + r) * D + col) = v;
+      }
+      if (!whole && threadIdx.x % TPW == 0) a.few_ml[place + r] = make_float2(top, sum);
+    }
   }
-  if (!whole && (threadIdx.x & 7) == 0) a.part_ml[part_row] = make_float2(top, sum);
 }
 
 // The sequence of token t, or -1: the last b with cu[b] <= t, by a search with 32 probes a step.
@@ -317,62 +494,125 @@ __device__ __forceinline__ int seq_of_token(const DenseArgs& a, int t) {
   return lo;
 }
 
-// Rows whose keys lie in more than one part: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p, a warp a row, in the order of the parts.
+// Rows whose keys were cut: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p over the pieces p, a CTA a row.  Its warps take the pieces in turn, four at a time
+// (a single sequence's row may lie in 296), and are added up in order.
+constexpr int kJoinWarps = 8;
+
 template <class T, int D>
-__global__ void __launch_bounds__(128) join_kernel(const DenseArgs a) {
-  chain_wait();
-  const int lane = threadIdx.x & 31;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + warp_index();
-  if (row >= static_cast<int64_t>(a.T) * a.H) return;
-  const int t = static_cast<int>(row / a.H), head = static_cast<int>(row % a.H), b = seq_of_token(a, t);
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const DenseArgs a) {
+  __shared__ float o_s[kJoinWarps][D];
+  __shared__ float2 ml_s[kJoinWarps];
+  // (cu and lens are there before chain_wait: the kernel before this one lets it start only once it has waited for those before itself, and writes neither)
+  const int lane = threadIdx.x & 31, warp = warp_index();
+  const int t = blockIdx.x / a.H, head = blockIdx.x % a.H, b = seq_of_token(a, t);
   DenseSeq s;
-  if (seq_of(a, b, s) <= 0 || t < s.t0 || t >= s.t0 + s.n || s.len <= a.chunk) return;
-  const int parts = (s.len - 1) / a.chunk + 1;
-  const int64_t step = static_cast<int64_t>(a.T) * a.H;
-  float top = -INFINITY;
-  for (int p = lane; p < parts; p += 32) top = fmaxf(top, __ldcg(a.part_ml + row + p * step).x);
-#pragma unroll
-  for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-  float sum = 0.f, o[D / 32];
+  const int found = seq_of(a, b, s);
+  chain_wait();
+  if (found <= 0 || t < s.t0 || t >= s.t0 + s.n) return;
+  const int64_t row = static_cast<int64_t>(t) * a.H + head;
+  const bool few = s.n * a.G <= a.few_rows;
+  int parts, first = 0, row_of_few = 0;
+  if (few) {
+    const int2 p = __ldcg(a.few_pieces + row);
+    if (p.y < 0) return;
+    first = p.x;
+    parts = p.y - p.x / 2 + 1;
+    row_of_few = (t - s.t0) * a.G + head % a.G;
+  } else {
+    if (a.parts == 1 || s.len <= a.chunk) return;
+    parts = (s.len - 1) / a.chunk + 1;
+  }
+  auto place = [&](int p) {                                        // row of few_o, or of part_o
+    return few ? static_cast<int64_t>(p == 0 ? first : 2 * (first / 2 + p)) * a.few_rows + row_of_few : row + p * (static_cast<int64_t>(a.T) * a.H);
+  };
+  const float* from = few ? a.few_o : a.part_o;
+  const float2* stat = few ? a.few_ml : a.part_ml;
+  float m = -INFINITY, l = 0.f, o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float2 ml = __ldcg(a.part_ml + row + p * step);
-    const float* src = a.part_o + (row + p * step) * D + lane * (D / 32);
-    float x[D / 32];
-    if constexpr (D == 128) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
-      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-    } else {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
-      x[0] = v.x; x[1] = v.y;
-    }
-    // (a part that the row sees nothing of has no rows in memory)
-    const bool none = ml.x == -INFINITY && ml.y == 0.f;
-    const float f = none ? 0.f : fast_exp2(ml.x - top);
-    sum = none ? sum : fmaf(ml.y, f, sum);
+  for (int p0 = warp; p0 < parts; p0 += 4 * kJoinWarps) {
+    float2 ml[4];
+    float x[4][D / 32];
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = none ? o[i] : fmaf(x[i], f, o[i]);
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + i * kJoinWarps;
+      ml[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) x[i][e] = 0.f;
+      if (p < parts) {
+        const int64_t at = place(p);
+        ml[i] = __ldcg(stat + at);
+        const float* src = from + at * D + lane * (D / 32);
+        if constexpr (D == 128) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+          x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+        } else {
+          const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+          x[i][0] = v.x; x[i][1] = v.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (ml[i].x == -INFINITY && ml[i].y == 0.f) continue;        // nothing of it is seen (and its row may not be in memory)
+      const float top = fmaxf(m, ml[i].x), f = m == -INFINITY && l == 0.f ? 0.f : fast_exp2(m - top), w = fast_exp2(ml[i].x - top);
+      m = top;
+      l = l * f + ml[i].y * w;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] = o[e] * f + x[i][e] * w;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) o_s[warp][lane * (D / 32) + e] = o[e];
+  if (lane == 0) ml_s[warp] = make_float2(m, l);
+  __syncthreads();
+  if (warp != 0) return;
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, ml_s[w].x);
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float2 ml = ml_s[w];
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;
+    const float f = fast_exp2(ml.x - top);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) o[e] = fmaf(o_s[w][lane * (D / 32) + e], f, o[e]);
   }
   store_cols<T, D>(static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts, lane, o, sum == 0.f ? 0.f : 1.f / sum);
 }
 
+// Rows that the kernel holds for a sequence of so many, 32 at most.
+int few_rows_of(int64_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+
+template <class T, int D>
+static int launch_few_t(const DenseArgs& a, cudaStream_t st) {
+  auto go = [&](auto rows) {
+    constexpr int NR = decltype(rows)::value;
+    const int r = ensure_dynamic_smem(reinterpret_cast<const void*>(&few_kernel<T, D, NR>), FewConf<D, NR>::total);
+    if (r != FASTAR_OK) return r;
+    return launch_chained(few_kernel<T, D, NR>, a.few_ctas, kFewThreads, FewConf<D, NR>::total, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+  };
+  return a.few_rows == 8 ? go(std::integral_constant<int, 1>{}) : a.few_rows == 16 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+}
+template <int D>
+static int few_ctas_t(int rows) {
+  return rows == 8 ? FewConf<D, 1>::CTAS : rows == 16 ? FewConf<D, 2>::CTAS : FewConf<D, 4>::CTAS;
+}
+int few_ctas_an_sm(int rows, int D) { return D == 128 ? few_ctas_t<128>(rows) : few_ctas_t<64>(rows); }
+
 int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st) {
-  const int64_t most = static_cast<int64_t>(a.max_new) * a.G, rows = most < a.few_rows ? most : a.few_rows;
-  const int row_tiles = static_cast<int>((rows + 15) / 16);
-  void (*kern)(DenseArgs, int) = fp16 ? (D == 128 ? few_kernel<__half, 128> : few_kernel<__half, 64>) : (D == 128 ? few_kernel<__nv_bfloat16, 128> : few_kernel<__nv_bfloat16, 64>);
-  const int smem = D == 128 ? FewSmem<128>::total : FewSmem<64>::total;
-  const int r = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
-  if (r != FASTAR_OK) return r;
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.B) * row_tiles), a.parts, a.KV);
-  return launch_chained(kern, grid, kFewThreads, smem, st, a, row_tiles) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+  if (fp16) return D == 128 ? launch_few_t<__half, 128>(a, st) : launch_few_t<__half, 64>(a, st);
+  return D == 128 ? launch_few_t<__nv_bfloat16, 128>(a, st) : launch_few_t<__nv_bfloat16, 64>(a, st);
 }
 
 int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(a.T) * a.H + 3) / 4));
+  const int64_t rows = static_cast<int64_t>(a.T) * a.H;
+  if (rows > INT32_MAX) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   void (*kern)(DenseArgs) = fp16 ? (D == 128 ? join_kernel<__half, 128> : join_kernel<__half, 64>) : (D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>);
-  return launch_chained(kern, grid, 128, 0, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+  return launch_chained(kern, static_cast<unsigned>(rows), 32 * kJoinWarps, 0, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
 }
 
 }  // namespace fastar

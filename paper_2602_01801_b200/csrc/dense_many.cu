@@ -50,9 +50,6 @@ struct ManyItem {
 __host__ __device__ constexpr uint32_t make_idesc_f16(int m, int n, int b_mn_major) {
   return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
-__device__ __forceinline__ void add_f16x2(float2& s, uint32_t b) {
-  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.f16 %0, l, %0; add.f32.f16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
-}
 __device__ __forceinline__ void sts128(uint32_t at, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -395,9 +392,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
           uint32_t o[8];
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            const uint32_t v = (&raw[p].x)[w];
-            o[2 * w] = e4m3x2_to_half2(v & 0xFFFFu);
-            o[2 * w + 1] = e4m3x2_to_half2(v >> 16);
+            e4m3x4_to_half2((&raw[p].x)[w], o[2 * w], o[2 * w + 1]);
           }
 #pragma unroll
           for (int w = 0; w < 8; ++w) {
@@ -565,7 +560,11 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   }
   if (*spoilt_s && warp < kMoveWarp) {
     const int last = min(it.rows, it.row0 + kRowsCta);
-    for (int r = it.row0 + warp; r < last; r += kMoveWarp) dense_row_whole<T, D, PAGED>(a, it.b, s.t0 + r / a.G, it.kvh * a.G + r % a.G, s, it.part);
+    for (int r = it.row0 + warp; r < last; r += kMoveWarp) {
+      const int tok = s.t0 + r / a.G, head = it.kvh * a.G + r % a.G;
+      const int64_t part_row = (static_cast<int64_t>(it.part) * a.T + tok) * a.H + head;
+      dense_row_to<T, D, PAGED>(a, it.b, tok, head, s, it.k0, whole ? s.len : it.k0 + a.chunk, whole, a.part_o + part_row * D, a.part_ml + part_row);
+    }
   }
 }
 

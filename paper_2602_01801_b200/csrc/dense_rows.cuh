@@ -28,6 +28,14 @@ __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
   asm("{.reg .b16 c; cvt.u16.u32 c, %1; cvt.rn.f16x2.e4m3x2 %0, c;}" : "=r"(r) : "r"(two));
   return r;
 }
+// The four codes of a word.
+__device__ __forceinline__ void e4m3x4_to_half2(uint32_t four, uint32_t& lo, uint32_t& hi) {
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}" : "=r"(lo), "=r"(hi) : "r"(four));
+}
+// Both halves of an fp16 pair to a sum each, as they are.
+__device__ __forceinline__ void add_f16x2(float2& s, uint32_t b) {
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.f16 %0, l, %0; add.f32.f16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
+}
 
 // D / 32 neighbouring columns of a row a lane.
 template <class T, int D>
@@ -97,21 +105,19 @@ __device__ __forceinline__ void store_cols(T* row, int lane, const float (&o)[D 
   if constexpr (D == 128) *reinterpret_cast<uint2*>(row + lane * 4) = make_uint2(narrow2<T>(o[0] * inv, o[1] * inv), narrow2<T>(o[2] * inv, o[3] * inv));
   else *reinterpret_cast<uint32_t*>(row + lane * 2) = narrow2<T>(o[0] * inv, o[1] * inv);
 }
+// (`whole`: all that the row sees is in [k0, k1), and it goes into `out`; otherwise a part of it, to part_o and part_ml.)
 template <class T, int D, bool PAGED>
-__device__ __forceinline__ void dense_row_whole(const DenseArgs& a, int b, int t, int head, const DenseSeq& s, int part) {
+__device__ __forceinline__ void dense_row_to(const DenseArgs& a, int b, int t, int head, const DenseSeq& s, int k0, int k1, bool whole, float* part_o, float2* part_ml) {
   const int lane = threadIdx.x & 31, end = visible_end(s.len - s.n + (t - s.t0), s.len, a.frame);
-  const bool whole = a.parts == 1 || s.len <= a.chunk;
-  const int k0 = whole ? 0 : part * a.chunk, k1 = whole ? end : min(end, k0 + a.chunk);
   float m, l, o[D / 32];
-  dense_row<T, D, PAGED>(a, b, t, head, s, k0, k1, m, l, o);
+  dense_row<T, D, PAGED>(a, b, t, head, s, k0, min(end, k1), m, l, o);
   if (whole) {
     // (a sum of NaN has to reach the row)
     store_cols<T, D>(static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts, lane, o, l == 0.f ? 0.f : 1.f / l);
   } else {
-    const int64_t row = (static_cast<int64_t>(part) * a.T + t) * a.H + head;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) a.part_o[row * D + lane * (D / 32) + i] = o[i];
-    if (lane == 0) a.part_ml[row] = make_float2(m, l);
+    for (int i = 0; i < D / 32; ++i) part_o[lane * (D / 32) + i] = o[i];
+    if (lane == 0) *part_ml = make_float2(m, l);
   }
 }
 

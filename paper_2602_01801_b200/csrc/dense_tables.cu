@@ -54,6 +54,7 @@ block_tables_kernel(const int32_t* __restrict__ held, const int32_t* __restrict_
   __shared__ int64_t red[66];
   __shared__ int granted_s;
   chain_wait();
+  chain_next();
   const int f0 = *first;
   const bool list_ok = f0 >= 0 && f0 <= n_free;
   const int avail = list_ok ? n_free - f0 : 0;
@@ -230,6 +231,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const Append
   __shared__ int found[2];
   __shared__ uint32_t most[4];
   chain_wait();
+  chain_next();
   // the item-th touched page of the call
   int64_t before = 0;
   const int64_t item = blockIdx.x;

@@ -115,11 +115,15 @@ _raw_stream = None
 def _stream() -> int:
     # The current stream's handle without a Stream object around it, which takes the host 3.4 us to make: three of a small step's 72.
     # torch has that only under a private name; where it is not there, through the object.
-    global _raw_stream
     import torch
     if _raw_stream is None:
-        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _find_raw_stream(torch)
     return _raw_stream(torch.cuda.current_device())
+
+
+def _find_raw_stream(torch) -> None:
+    global _raw_stream
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 class Cache:
@@ -423,131 +427,124 @@ def noalloc_last_status() -> int:
 # ---- the dense path of several rollouts -----------------------------------------------------------
 # Packed sequences: tokens [cu[b], cu[b+1]) of [head][T][d] belong to sequence b.  The 8-bit cache: code pools [pages][kv heads][page tokens][d] (uint8,
 # fp8 e4m3 codes) with scales [pages][kv heads] (fp32), and a table [sequences][width] of pages.  Full rules: include/fastar.h.
-_dense_dtypes = None
+# A call of these takes the GPU a few microseconds at the smallest, so what the host does for one counts: tensors are looked at once each, by the
+# cheapest of their attributes.
+_dense = None                # (library, torch, dtype codes, int32, uint8, float32, current device), once it is loaded
 
 
-def _need(ok: bool, where: str) -> None:
-    if not ok:
-        raise FastarError(ERR_INVALID_ARG, where)
-
-
-def _rows(t, where: str):
-    """(dtype code, head stride, token stride) of a packed tensor [head][T][d]."""
-    global _dense_dtypes
-    if _dense_dtypes is None:
-        import torch
-        _dense_dtypes = {torch.bfloat16: BF16, torch.float16: FP16}
-    dtype = _dense_dtypes.get(t.dtype)
-    _need(dtype is not None and t.dim() == 3 and t.is_cuda and (t.stride(2) == 1 or t.shape[2] == 1), where)
-    return dtype, t.stride(0), t.stride(1)
-
-
-def _ints(where: str, device, *tensors) -> None:
+def _dense_init():
+    global _dense
     import torch
+    if _raw_stream is None:
+        _find_raw_stream(torch)
+    _dense = (load_library(), torch, {torch.bfloat16: BF16, torch.float16: FP16}, torch.int32, torch.uint8, torch.float32, torch.cuda.current_device)
+    return _dense
+
+
+def _refuse(where: str):
+    raise FastarError(ERR_INVALID_ARG, where)
+
+
+def _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale) -> bool:
+    P, KV = k_codes.shape[0], k_codes.shape[1]
+    u8, f32 = torch.uint8, torch.float32
+    return (k_codes.dtype == u8 and v_codes.dtype == u8 and k_scale.dtype == f32 and v_scale.dtype == f32 and k_codes.get_device() == dev and v_codes.get_device() == dev
+            and k_scale.get_device() == dev and v_scale.get_device() == dev and k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
+            and v_scale.is_contiguous() and v_codes.shape == k_codes.shape and k_scale.shape == (P, KV) and v_scale.shape == (P, KV))
+
+
+def _ints_ok(i32, dev, *tensors) -> bool:
     for t in tensors:
-        _need(t.dtype == torch.int32 and t.device == device and t.is_contiguous(), where)
+        if t.dtype != i32 or t.get_device() != dev or not t.is_contiguous():
+            return False
+    return True
 
 
-class _on:
-    """The tensors' device as the current one, at no cost where it is already."""
-
-    def __init__(self, device):
-        self.device, self.guard = device, None
-
-    def __enter__(self):
-        import torch
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _out_like(torch, q, strides, out, where):
+    if out is None:
+        out = torch.empty_like(q)
+        return out if out.stride() == strides else torch.empty_strided(q.shape, strides, dtype=q.dtype, device=q.device)
+    if out.dtype != q.dtype or out.get_device() != q.get_device() or out.shape != q.shape or out.stride() != strides:
+        _refuse(where)
+    return out
 
 
 def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add: int) -> Dict[str, "object"]:
     """Page tables and slots on the GPU from the requests' lengths: held, add [B] int32, the free list free_pages[first:] and table [B][W], whose new
     entries are written in place.  Returns cu [B+1], lens [B] (-1: refused), slots [max_add] int64 and first [1], where the free list goes on."""
-    import torch
-    where, dev = "block_tables", held.device
-    _need(held.is_cuda and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and first.numel() == 1 and max_add >= 0, where)
-    _ints(where, dev, held, add, free_pages, first, table)
+    lib, torch, _, i32, _, _, current = _dense or _dense_init()
+    where, dev = "block_tables", held.get_device()
+    if not (dev >= 0 and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and first.numel() == 1 and max_add >= 0
+            and _ints_ok(i32, dev, held, add, free_pages, first, table)):
+        _refuse(where)
+    if dev != current():
+        with torch.cuda.device(dev):
+            return block_tables(held, add, page_tokens, free_pages, first, table, max_add)
     B = held.shape[0]
-    with _on(dev):
-        cu_lens = torch.empty(2 * B + 2, dtype=torch.int32, device=dev)
-        slots = torch.empty(max_add, dtype=torch.int64, device=dev)
-        r = dict(cu=cu_lens[: B + 1], lens=cu_lens[B + 1: 2 * B + 1], slots=slots, first=cu_lens[2 * B + 1:])
-        _check(load_library().fastar_block_tables(held.data_ptr(), add.data_ptr(), B, page_tokens, free_pages.data_ptr(), free_pages.numel(), first.data_ptr(),
-                                                  table.data_ptr(), table.shape[1], r["cu"].data_ptr(), r["lens"].data_ptr(), slots.data_ptr(), max_add,
-                                                  r["first"].data_ptr(), _stream()), "fastar_block_tables")
-    return r
-
-
-def _pools(where, device, k_codes, v_codes, k_scale, v_scale):
-    import torch
-    P, KV, PT, D = k_codes.shape
-    for t in (k_codes, v_codes):
-        _need(t.dtype == torch.uint8 and t.device == device and t.is_contiguous() and tuple(t.shape) == (P, KV, PT, D), where)
-    for t in (k_scale, v_scale):
-        _need(t.dtype == torch.float32 and t.device == device and t.is_contiguous() and tuple(t.shape) == (P, KV), where)
-    return P, KV, PT, D
+    cu, lens, first_out = torch.empty(2 * B + 2, dtype=i32, device=held.device).split((B + 1, B, 1))
+    slots = torch.empty(max_add, dtype=torch.int64, device=held.device)
+    _check(lib.fastar_block_tables(held.data_ptr(), add.data_ptr(), B, page_tokens, free_pages.data_ptr(), free_pages.shape[0], first.data_ptr(), table.data_ptr(),
+                                   table.shape[1], cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), max_add, first_out.data_ptr(), _raw_stream(dev)), "fastar_block_tables")
+    return dict(cu=cu, lens=lens, slots=slots, first=first_out)
 
 
 def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu) -> None:
     """Writes the packed rows k_new, v_new [KV][T][d] into the 8-bit pages: token i of sequence b to position lens[b] - n_b + i."""
-    where, dev = "kv8_append", k_new.device
-    dtype, hs, ts = _rows(k_new, where)
-    _need(_rows(v_new, where) == (dtype, hs, ts) and v_new.shape == k_new.shape and v_new.device == dev, where)
-    P, KV, PT, D = _pools(where, dev, k_codes, v_codes, k_scale, v_scale)
-    B = lens.shape[0]
-    _need(k_new.shape[0] == KV and k_new.shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and tuple(cu.shape) == (B + 1,), where)
-    _ints(where, dev, table, lens, cu)
-    with _on(dev):
-        _check(load_library().fastar_kv8_append(k_new.data_ptr(), v_new.data_ptr(), hs, ts, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
-                                                P, PT, table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, k_new.shape[1], KV, D, dtype, _stream()),
-               "fastar_kv8_append")
+    lib, torch, dtypes, i32, _, _, current = _dense or _dense_init()
+    where, dev = "kv8_append", k_new.get_device()
+    dtype, shape, strides = dtypes.get(k_new.dtype), k_new.shape, k_new.stride()
+    if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and v_new.dtype == k_new.dtype and v_new.shape == shape and v_new.stride() == strides
+            and v_new.get_device() == dev and k_codes.dim() == 4 and _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale)):
+        _refuse(where)
+    (P, KV, PT, D), B = k_codes.shape, lens.shape[0]
+    if not (shape[0] == KV and shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and cu.shape == (B + 1,) and _ints_ok(i32, dev, table, lens, cu)):
+        _refuse(where)
+    if dev != current():
+        with torch.cuda.device(dev):
+            return kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu)
+    _check(lib.fastar_kv8_append(k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                 P, PT, table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, shape[1], KV, D, dtype, _raw_stream(dev)), "fastar_kv8_append")
 
 
 def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new: int, max_len: int, frame_len: int = 1, out=None):
     """Attention of the packed new tokens q [H][T][d] over the 8-bit cache, which holds their own keys already; n_b <= max_new, lens[b] <= max_len.
     frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  Returns out (rows of no sequence are left as they were)."""
-    import torch
-    where, dev = "kv8_attention", q.device
-    dtype, hs, ts = _rows(q, where)
-    P, KV, PT, D = _pools(where, dev, k_codes, v_codes, k_scale, v_scale)
-    (H, T, _), B = q.shape, lens.shape[0]
-    _need(q.shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and tuple(cu.shape) == (B + 1,), where)
-    _ints(where, dev, table, lens, cu)
-    if out is None:
-        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)
-    _need(_rows(out, where) == (dtype, hs, ts) and out.shape == q.shape and out.device == dev, where)
-    lib = load_library()
-    with _on(dev):
-        nbytes = lib.fastar_kv8_attention_workspace_bytes(B, T, max_new, max_len, H, KV, D)
-        work = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        _check(lib.fastar_kv8_attention(q.data_ptr(), out.data_ptr(), hs, ts, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
-                                        table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
-                                        work.data_ptr(), nbytes, _stream()), "fastar_kv8_attention")
+    lib, torch, dtypes, i32, u8, _, current = _dense or _dense_init()
+    where, dev = "kv8_attention", q.get_device()
+    dtype, shape, strides = dtypes.get(q.dtype), q.shape, q.stride()
+    if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and k_codes.dim() == 4 and _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale)):
+        _refuse(where)
+    (P, KV, PT, D), (H, T, d), B = k_codes.shape, shape, lens.shape[0]
+    if not (d == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and cu.shape == (B + 1,) and _ints_ok(i32, dev, table, lens, cu)):
+        _refuse(where)
+    if dev != current():
+        with torch.cuda.device(dev):
+            return kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new, max_len, frame_len, out)
+    out = _out_like(torch, q, strides, out, where)
+    nbytes = lib.fastar_kv8_attention_workspace_bytes(B, T, max_new, max_len, H, KV, D)
+    work = torch.empty(nbytes, dtype=u8, device=q.device)
+    _check(lib.fastar_kv8_attention(q.data_ptr(), out.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
+                                    table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
+                                    work.data_ptr(), nbytes, _raw_stream(dev)), "fastar_kv8_attention")
     return out
 
 
 def packed_attention(q, k, v, cu, max_tokens: int, frame_len: int = 1, out=None):
     """Attention of packed sequences over their own tokens: q [H][T][d], k and v [KV][T][d], H a multiple of KV; no sequence is longer than max_tokens.
     frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  Returns out (rows of no sequence are left as they were)."""
-    import torch
-    where, dev = "packed_attention", q.device
-    dtype, hs, ts = _rows(q, where)
-    kd, khs, kts = _rows(k, where)
-    _need(kd == dtype and _rows(v, where) == (kd, khs, kts) and v.shape == k.shape and k.device == dev and v.device == dev, where)
-    (H, T, D), KV = q.shape, k.shape[0]
-    _need(k.shape[1] == T and k.shape[2] == D and cu.dim() == 1 and cu.shape[0] >= 2, where)
-    _ints(where, dev, cu)
-    if out is None:
-        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)
-    _need(_rows(out, where) == (dtype, hs, ts) and out.shape == q.shape and out.device == dev, where)
-    with _on(dev):
-        _check(load_library().fastar_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), hs, ts, khs, kts, cu.data_ptr(), cu.shape[0] - 1, T,
-                                                      max_tokens, H, KV, D, dtype, frame_len, _stream()), "fastar_packed_attention")
+    lib, torch, dtypes, i32, _, _, current = _dense or _dense_init()
+    where, dev = "packed_attention", q.get_device()
+    dtype, shape, strides, kv_shape, kv_strides = dtypes.get(q.dtype), q.shape, q.stride(), k.shape, k.stride()
+    if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and len(kv_shape) == 3 and kv_strides[2] == 1 and k.dtype == q.dtype and v.dtype == q.dtype
+            and v.shape == kv_shape and v.stride() == kv_strides and k.get_device() == dev and v.get_device() == dev and kv_shape[1:] == shape[1:]
+            and cu.dim() == 1 and cu.shape[0] >= 2 and _ints_ok(i32, dev, cu)):
+        _refuse(where)
+    if dev != current():
+        with torch.cuda.device(dev):
+            return packed_attention(q, k, v, cu, max_tokens, frame_len, out)
+    out = _out_like(torch, q, strides, out, where)
+    _check(lib.fastar_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), strides[0], strides[1], kv_strides[0], kv_strides[1], cu.data_ptr(),
+                                       cu.shape[0] - 1, shape[1], max_tokens, shape[0], kv_shape[0], shape[2], dtype, frame_len, _raw_stream(dev)), "fastar_packed_attention")
     return out
 
 
