@@ -494,22 +494,23 @@ __device__ __forceinline__ int seq_of_token(const DenseArgs& a, int t) {
   return lo;
 }
 
-// Rows whose keys were cut: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p over the pieces p, a CTA a row.  Its warps take the pieces in turn, four at a time
-// (a single sequence's row may lie in 296), and are added up in order.
-constexpr int kJoinWarps = 8;
+// Rows whose keys were cut: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p over the pieces p.  WARPS warps a row take its pieces in turn, four at a time, and are
+// added up in order: eight where there are few rows, each of which may lie in hundreds of pieces, one where there are many.
+constexpr int kJoinThreads = 256;
 
-template <class T, int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const DenseArgs a) {
-  __shared__ float o_s[kJoinWarps][D];
-  __shared__ float2 ml_s[kJoinWarps];
+template <class T, int D, int WARPS>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
+  __shared__ float o_s[WARPS][D];
+  __shared__ float2 ml_s[WARPS];
   // (cu and lens are there before chain_wait: the kernel before this one lets it start only once it has waited for those before itself, and writes neither)
-  const int lane = threadIdx.x & 31, warp = warp_index();
-  const int t = blockIdx.x / a.H, head = blockIdx.x % a.H, b = seq_of_token(a, t);
+  const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : warp_index();
+  const int64_t row = WARPS == 1 ? static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + warp_index() : blockIdx.x;
+  if (row >= static_cast<int64_t>(a.T) * a.H) return;              // (a whole CTA, or a warp of its own)
+  const int t = static_cast<int>(row / a.H), head = static_cast<int>(row - static_cast<int64_t>(t) * a.H), b = seq_of_token(a, t);
   DenseSeq s;
   const int found = seq_of(a, b, s);
   chain_wait();
   if (found <= 0 || t < s.t0 || t >= s.t0 + s.n) return;
-  const int64_t row = static_cast<int64_t>(t) * a.H + head;
   const bool few = s.n * a.G <= a.few_rows;
   int parts, first = 0, row_of_few = 0;
   if (few) {
@@ -530,12 +531,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const DenseArgs a
   float m = -INFINITY, l = 0.f, o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
-  for (int p0 = warp; p0 < parts; p0 += 4 * kJoinWarps) {
+  for (int p0 = warp; p0 < parts; p0 += 4 * WARPS) {
     float2 ml[4];
     float x[4][D / 32];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int p = p0 + i * kJoinWarps;
+      const int p = p0 + i * WARPS;
       ml[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) x[i][e] = 0.f;
@@ -562,26 +563,29 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const DenseArgs a
       for (int e = 0; e < D / 32; ++e) o[e] = o[e] * f + x[i][e] * w;
     }
   }
+  if constexpr (WARPS > 1) {
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) o_s[warp][lane * (D / 32) + e] = o[e];
-  if (lane == 0) ml_s[warp] = make_float2(m, l);
-  __syncthreads();
-  if (warp != 0) return;
-  float top = -INFINITY, sum = 0.f;
+    for (int e = 0; e < D / 32; ++e) o_s[warp][lane * (D / 32) + e] = o[e];
+    if (lane == 0) ml_s[warp] = make_float2(m, l);
+    __syncthreads();
+    if (warp != 0) return;
+    float top = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, ml_s[w].x);
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml_s[w].x);
+    l = 0.f;
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+    for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
 #pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) {
-    const float2 ml = ml_s[w];
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;
-    const float f = fast_exp2(ml.x - top);
-    sum = fmaf(ml.y, f, sum);
+    for (int w = 0; w < WARPS; ++w) {
+      const float2 ml = ml_s[w];
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;
+      const float f = fast_exp2(ml.x - top);
+      l = fmaf(ml.y, f, l);
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] = fmaf(o_s[w][lane * (D / 32) + e], f, o[e]);
+      for (int e = 0; e < D / 32; ++e) o[e] = fmaf(o_s[w][lane * (D / 32) + e], f, o[e]);
+    }
   }
-  store_cols<T, D>(static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts, lane, o, sum == 0.f ? 0.f : 1.f / sum);
+  store_cols<T, D>(static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts, lane, o, l == 0.f ? 0.f : 1.f / l);
 }
 
 // Rows that the kernel holds for a sequence of so many, 32 at most.
@@ -608,11 +612,17 @@ int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st) {
   return D == 128 ? launch_few_t<__nv_bfloat16, 128>(a, st) : launch_few_t<__nv_bfloat16, 64>(a, st);
 }
 
-int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st) {
+template <class T, int D>
+static int launch_join_t(const DenseArgs& a, cudaStream_t st) {
   const int64_t rows = static_cast<int64_t>(a.T) * a.H;
   if (rows > INT32_MAX) return FASTAR_ERR_UNSUPPORTED_SHAPE;
-  void (*kern)(DenseArgs) = fp16 ? (D == 128 ? join_kernel<__half, 128> : join_kernel<__half, 64>) : (D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>);
-  return launch_chained(kern, static_cast<unsigned>(rows), 32 * kJoinWarps, 0, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+  const bool few = rows < 4096;                                    // eight warps a row are as many as the SMs hold at once then
+  const unsigned grid = static_cast<unsigned>(few ? rows : (rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
+  return launch_chained(few ? join_kernel<T, D, 8> : join_kernel<T, D, 1>, grid, kJoinThreads, 0, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+}
+int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st) {
+  if (fp16) return D == 128 ? launch_join_t<__half, 128>(a, st) : launch_join_t<__half, 64>(a, st);
+  return D == 128 ? launch_join_t<__nv_bfloat16, 128>(a, st) : launch_join_t<__nv_bfloat16, 64>(a, st);
 }
 
 }  // namespace fastar

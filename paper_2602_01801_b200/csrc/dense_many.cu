@@ -337,88 +337,107 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       if (lane == 0) unit_s[warp - kMoveWarp] = most;
       named_barrier_sync(1, 128);
       most = fmaxf(fmaxf(unit_s[0], unit_s[1]), fmaxf(unit_s[2], unit_s[3]));
-      // Units of work: K(0), then K(j + 1) and V(j) in turn.  The codes of the next one are on their way while one is converted.
+      // Units of work: K(0), then K(j + 1) and V(j) in turn.  While one is converted the codes of the next are on their way, and those of the one after it are asked
+      // for piece by piece, where its own have been used.
       constexpr int TPR = D / 16, RPP = 128 / TPR, PASSES = 128 / RPP;           // threads a row, rows a pass
       const int c = tid % TPR, r0 = tid / TPR;
       int window = -64, window_page = 0;
       __half2 nan_seen = __float2half2_rn(0.f);
-      auto unit_of = [&](int u, bool& is_v, int& j) {              // false: past the end
-        is_v = u > 0 && (u & 1) == 0;
-        j = u == 0 ? 0 : is_v ? u / 2 - 1 : (u + 1) / 2;
-        return j < nt;
-      };
       const int units = 2 * nt + 1;                                // (K(nt) is none)
-      auto ask = [&](int u, uint4 (&raw)[PASSES], float2& scale) {
-        bool is_v;
-        int j;
-        if (u >= units || !unit_of(u, is_v, j)) return;
-        const int key0 = it.k0 + j * kKeys;
-        const int p0 = key0 / a.PT, p1 = a.PT == 64 && key0 + 64 < it.see ? p0 + 1 : p0;
-        if (p1 - window >= 32 || window < 0 || p0 < window) {
-          window = p0;
-          window_page = p0 + lane < n_pages ? page_of(a, it.b, p0 + lane) : 0;
-        }
-        const int64_t at0 = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p0 - window)) * a.KV + it.kvh;
-        const int64_t at1 = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p1 - window)) * a.KV + it.kvh;
-        const uint8_t* codes = is_v ? a.vc : a.kc;
-        const float* scales = is_v ? a.vs : a.ks;
-        scale = make_float2(scales[at0], scales[at1]);
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-          const int row = p * RPP + r0;
-          const bool second = a.PT == 64 && row >= 64;
-          const int64_t off = ((second ? at1 : at0) * a.PT + (second ? row - 64 : row)) * D + c * 16;
-          raw[p] = key0 + row < it.see ? __ldg(reinterpret_cast<const uint4*>(codes + off)) : make_uint4(0u, 0u, 0u, 0u);
-        }
+      struct Unit {
+        bool there, is_v, full;
+        int j, left;                                               // its tile; rows of it that are seen
+        const uint8_t *at0, *at1;                                  // this thread's codes in the first and the second 64 rows
+        float2 scale;
       };
-      auto convert = [&](int u, const uint4 (&raw)[PASSES], float2 scale) {
-        bool is_v;
-        int j;
-        if (!unit_of(u, is_v, j)) return true;
-        const int st = is_v ? j % SV : j % SK, n = is_v ? SV : SK;
-        const uint32_t full = (is_v ? bar_v_full : bar_k_full) + 8 * st, empty = (is_v ? bar_v_empty : bar_k_empty) + 8 * st;
-        if (j >= n && !mbar_wait_warp<kIssueWaitHintNs>(empty, (j / n - 1) & 1, abort_flag, a.status)) return false;
-        const uint32_t tile = sbase + (is_v ? SM::v_off : SM::k_off) + st * SM::q_tile;
-        const float f0 = is_v ? scale.x / most : 1.f, f1 = is_v ? scale.y / most : 1.f;
-        if (is_v) {
-          // (2^-126 is the scale of a page of zeros)
-          if ((f0 < 3.0517578e-5f && scale.x > 1.17549435e-38f) || (f1 < 3.0517578e-5f && scale.y > 1.17549435e-38f)) spoilt = true;
+      auto find = [&](int u) {
+        Unit w;
+        w.is_v = u > 0 && (u & 1) == 0;
+        w.j = u == 0 ? 0 : w.is_v ? u / 2 - 1 : (u + 1) / 2;
+        w.there = u < units && w.j < nt;
+        w.scale = make_float2(0.f, 0.f);
+        w.at0 = w.at1 = nullptr;
+        w.left = 0;
+        if (w.there) {
+          const int key0 = it.k0 + w.j * kKeys;
+          w.left = it.see - key0;
+          const int p0 = key0 / a.PT, p1 = a.PT == 64 && w.left > 64 ? p0 + 1 : p0;
+          if (p1 - window >= 32 || window < 0 || p0 < window) {
+            window = p0;
+            window_page = p0 + lane < n_pages ? page_of(a, it.b, p0 + lane) : 0;
+          }
+          const int64_t at0 = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p0 - window)) * a.KV + it.kvh;
+          const int64_t at1 = static_cast<int64_t>(__shfl_sync(0xffffffffu, window_page, p1 - window)) * a.KV + it.kvh;
+          const uint8_t* codes = w.is_v ? a.vc : a.kc;
+          const float* scales = w.is_v ? a.vs : a.ks;
+          w.scale = make_float2(scales[at0], scales[at1]);
+          w.at0 = codes + at0 * a.PT * D + tid * 16;
+          w.at1 = a.PT == 64 ? codes + at1 * a.PT * D + tid * 16 - 64 * D : w.at0;
         }
+        return w;
+      };
+      auto ask = [&](const Unit& w, int p) {                       // RPP rows x D codes are 2048 bytes
+        const uint8_t* at = (p < PASSES / 2 ? w.at0 : w.at1) + p * 2048;
+        return w.there && p * RPP + r0 < w.left ? __ldg(reinterpret_cast<const uint4*>(at)) : make_uint4(0u, 0u, 0u, 0u);
+      };
+      auto convert = [&](const Unit& w, uint4 (&raw)[PASSES], const Unit& next) {
+        if (!w.there) return true;                                 // (K(nt) only: behind it there is V(nt - 1), which has been asked for)
+        const int st = w.is_v ? w.j % SV : w.j % SK, n = w.is_v ? SV : SK;
+        const uint32_t full = (w.is_v ? bar_v_full : bar_k_full) + 8 * st, empty = (w.is_v ? bar_v_empty : bar_k_empty) + 8 * st;
+        if (w.j >= n && !mbar_wait_warp<kIssueWaitHintNs>(empty, (w.j / n - 1) & 1, abort_flag, a.status)) return false;
+        const uint32_t tile = sbase + (w.is_v ? SM::v_off : SM::k_off) + st * SM::q_tile;
+        const float f0 = w.is_v ? w.scale.x / most : 1.f, f1 = w.is_v ? w.scale.y / most : 1.f;
+        // (2^-126 is the scale of a page of zeros)
+        if ((f0 < 3.0517578e-5f && w.scale.x > 1.17549435e-38f) || (f1 < 3.0517578e-5f && w.scale.y > 1.17549435e-38f)) spoilt = true;
         const __half2 h0 = __float2half2_rn(f0), h1 = __float2half2_rn(f1);
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-          const int row = p * RPP + r0;
-          const __half2 f = a.PT == 64 && row >= 64 ? h1 : h0;
+        const int first = D == 128 ? c >> 2 : 0;                   // which of its two pieces a thread stores first: eight lanes, eight banks
+        auto pass = [&](int p, auto look) {
           uint32_t o[8];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            e4m3x4_to_half2((&raw[p].x)[w], o[2 * w], o[2 * w + 1]);
-          }
+          for (int e = 0; e < 4; ++e) e4m3x4_to_half2((&raw[p].x)[e], o[2 * e], o[2 * e + 1]);
+          raw[p] = ask(next, p);
+          if (decltype(look)::value) {
+            const __half2 f = p < PASSES / 2 ? h0 : h1;
 #pragma unroll
-          for (int w = 0; w < 8; ++w) {
-            __half2& h = *reinterpret_cast<__half2*>(&o[w]);
-            nan_seen = __hmax2_nan(nan_seen, h);
-            if (is_v) h = __hmul2(h, f);
+            for (int e = 0; e < 8; ++e) {
+              __half2& h = *reinterpret_cast<__half2*>(&o[e]);
+              nan_seen = __hmax2_nan(nan_seen, h);
+              h = __hmul2(h, f);
+            }
           }
-          const int first = D == 128 ? c >> 2 : 0;                 // which of its two pieces a thread stores first: eight lanes, eight banks
+          const int row = p * RPP + r0;
           const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
           sts128(tile + tile_at16(row, 2 * c + first), first ? hi : lo);
           sts128(tile + tile_at16(row, 2 * c + 1 - first), first ? lo : hi);
+        };
+        // Most tiles are seen by all rows, so that NaN codes go where they have to, and most pages have the largest scale
+        if (w.j < clean_from && f0 == 1.f && f1 == 1.f) {
+#pragma unroll
+          for (int p = 0; p < PASSES; ++p) pass(p, std::false_type{});
+        } else {
+#pragma unroll
+          for (int p = 0; p < PASSES; ++p) pass(p, std::true_type{});
         }
-        if (!is_v && tid == 0) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sbase + SM::scale_off + (j & 7) * 8), "f"(scale.x), "f"(scale.y) : "memory");
+        if (!w.is_v && tid == 0)
+          asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sbase + SM::scale_off + (w.j & 7) * 8), "f"(w.scale.x), "f"(w.scale.y) : "memory");
         fence_proxy_async_smem();
         mbar_arrive_warp(full);
         return true;
       };
-      uint4 ra[PASSES], rb[PASSES];
-      float2 sa = make_float2(0.f, 0.f), sb = make_float2(0.f, 0.f);
       if (nt > 0) {
-        ask(0, ra, sa);
+        uint4 ra[PASSES], rb[PASSES];
+        Unit ua = find(0), ub = find(1);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) ra[p] = ask(ua, p);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) rb[p] = ask(ub, p);
         for (int u = 0; u < units; u += 2) {
-          ask(u + 1, rb, sb);
-          if (!convert(u, ra, sa)) break;
-          ask(u + 2, ra, sa);
-          if (u + 1 < units && !convert(u + 1, rb, sb)) break;
+          const Unit na = find(u + 2);
+          if (!convert(ua, ra, na)) break;
+          ua = na;
+          const Unit nb = find(u + 3);
+          if (!convert(ub, rb, nb)) break;
+          ub = nb;
         }
       }
       spoilt |= __hisnan(__low2half(nan_seen)) || __hisnan(__high2half(nan_seen));
