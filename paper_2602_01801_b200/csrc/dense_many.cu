@@ -22,18 +22,29 @@
 
 namespace fastar {
 
-constexpr int kManyThreads = 512, kMoveWarp = 8, kMmaWarp = 12, kKWarp = 13, kVWarp = 14;
+constexpr int kManyThreads = 512, kMoveWarp = 8, kMmaWarp = 12, kKWarp = 14, kVWarp = 15;
 constexpr int kRowsCta = 256, kKeys = 128;
-// Registers a thread, dealt anew by role: 512 x 128 at launch = 256 x 184 + 128 x 96 + 128 x 48
-constexpr int kSoftmaxRegs = 184, kMoveRegs = 96, kRestRegs = 48;
+// The keys of a Q K^T and soft-max, and the registers a thread, dealt anew by role from 512 x 128 at launch: soft-max 256, movers 128, the rest 128 threads.
+template <int D>
+struct ManyRoles {
+  static constexpr int kSub = D == 128 ? 64 : 128;
+  static constexpr int kSoftmax = D == 128 ? 152 : 184, kMove = D == 128 ? 144 : 96, kRest = D == 128 ? 64 : 48;
+  static_assert(2 * kSoftmax + kMove + kRest <= 4 * 128, "what rises takes what falls gives");
+};
+template <int N>
+__device__ __forceinline__ void set_regs() {
+  if constexpr (N > 128) setmaxnreg_inc<N>();
+  else if constexpr (N < 128) setmaxnreg_dec<N>();
+}
 constexpr float kRaise = 8.f;
+constexpr int kPoly = 3;                                          // pairs of every 16 whose exponentials the FMA units work out
 
 template <int D>
 struct ManySmem {
   static constexpr int q_tile = (D / 64) * 128 * 128;              // bytes of a query tile, and of a K or V tile
   static constexpr int SK = D == 128 ? 3 : 4, SV = D == 128 ? 2 : 4;
   static constexpr int k_off = 2 * q_tile, v_off = k_off + SK * q_tile, bar_off = v_off + SV * q_tile;
-  static constexpr int scale_off = bar_off + 256;                  // [8][2] key scales of a tile's two halves
+  static constexpr int scale_off = bar_off + 512;                  // [8][2] key scales of a tile's two halves
   static constexpr int misc_off = scale_off + 64;
   static constexpr int factor_off = misc_off + 64;                 // [256]
   static constexpr int total = factor_off + 1024;
@@ -62,6 +73,8 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   using SM = ManySmem<D>;
   using M = typename std::conditional<PAGED, __half, T>::type;     // the products' type
   constexpr bool kHalf = std::is_same<M, __half>::value;
+  constexpr bool kOver = D == 128;                                 // P lies over S: there is no more room in tensor memory
+  constexpr int kSub = ManyRoles<D>::kSub, NS = kKeys / kSub;      // parts of a key tile
   constexpr int SK = SM::SK, SV = SM::SV;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
@@ -71,10 +84,11 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   }
   const uint32_t bar = sbase + SM::bar_off;
   const uint32_t bar_q = bar, bar_k_full = bar + 8, bar_k_empty = bar_k_full + 8 * SK, bar_v_full = bar_k_empty + 8 * SK, bar_v_empty = bar_v_full + 8 * SV;
-  const uint32_t bar_v_clean = bar_v_empty + 8 * SV, bar_v_asked = bar_v_clean + 8 * SV, bar_s = bar_v_asked + 8 * SV, bar_p = bar_s + 16, bar_pv = bar_p + 16;
-  const uint32_t bar_drain = bar_pv + 16;
-  constexpr int kNumBars = 1 + 2 * SK + 4 * SV + 7;
-  static_assert(kNumBars * 8 <= 256, "barriers");
+  const uint32_t bar_v_clean = bar_v_empty + 8 * SV, bar_v_asked = bar_v_clean + 8 * SV;
+  // [query tile][half of the keys] each: logits; they are in registers; probabilities; P V
+  const uint32_t bar_s = bar_v_asked + 8 * SV, bar_ld = bar_s + 32, bar_p = bar_ld + 32, bar_pv = bar_p + 32, bar_drain = bar_pv + 32;
+  constexpr int kRoleBars = 1 + 2 * SK + 4 * SV, kNumBars = kRoleBars + 18;
+  static_assert(kNumBars * 8 <= 512, "barriers");
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::misc_off);
   volatile int* spoilt_s = abort_flag + 1;
   volatile int* done_flag = abort_flag + 2;                        // stays 0
@@ -154,10 +168,10 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   const int clean_from = it.nt[1] > 0 ? (it.nt[0] > 0 ? min(it.whole_from[0], it.whole_from[1]) : it.whole_from[1]) : it.whole_from[0];
 
   if (threadIdx.x < kNumBars) {
-    const int i = threadIdx.x;
-    // q; k_full, k_empty; v_full, v_empty, v_clean, v_asked; s, p, pv (two each), drain
-    const int count = i == 0 ? 4 : i < 1 + SK ? (PAGED ? 4 : 1) : i < 1 + 2 * SK ? 1 : i < 1 + 2 * SK + SV ? (PAGED ? 4 : 1) : i < 1 + 2 * SK + 2 * SV ? 1
-                      : i < 1 + 2 * SK + 3 * SV ? 4 : i < 1 + 2 * SK + 4 * SV ? 1 : i < 3 + 2 * SK + 4 * SV ? 2 : i < 5 + 2 * SK + 4 * SV ? 4 : 1;
+    const int i = threadIdx.x, role = i - kRoleBars;
+    // q; k_full, k_empty; v_full, v_empty, v_clean, v_asked; s, ld, p, pv, drain
+    const int count = i == 0 ? 4 : i < 1 + SK ? (PAGED ? 4 : 1) : i < 1 + 2 * SK ? 2 : i < 1 + 2 * SK + SV ? (PAGED ? 4 : 1) : i < 1 + 2 * SK + 2 * SV ? 2
+                      : i < 1 + 2 * SK + 3 * SV ? 4 : role < 0 ? 1 : role < 4 ? 2 : role < 12 ? 4 : 1;
     mbar_init(bar + 8 * i, count);
     fence_mbar_init();
   }
@@ -173,58 +187,80 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  chain_next();
 
   if (warp >= kMmaWarp) {
-    setmaxnreg_dec<kRestRegs>();
-    if (warp == kMmaWarp) {
-      // ================================================================ MMAs
+    set_regs<ManyRoles<D>::kRest>();
+    if (warp < kKWarp) {
+      // ================================================================ MMAs of query tile t
+      const int t = warp - kMmaWarp, n = it.nt[t];
       const uint32_t lead = elect_lane();
-      constexpr uint32_t id_s = kHalf ? make_idesc_f16(128, kKeys, 0) : make_idesc_bf16(128, kKeys, 0);
+      constexpr uint32_t id_s = kHalf ? make_idesc_f16(128, kSub, 0) : make_idesc_bf16(128, kSub, 0);
       constexpr uint32_t id_o = kHalf ? make_idesc_f16(128, D, 1) : make_idesc_bf16(128, D, 1);
-      const uint64_t qd = make_smem_desc(sbase, 16, 1024), kd = make_smem_desc(sbase + SM::k_off, 16, 1024), vd = make_smem_desc(sbase + SM::v_off, 16384, 1024);
-      bool ok = nt > 0 && mbar_wait_warp<kIssueWaitHintNs>(bar_q, 0, abort_flag, a.status);
-      auto scores = [&](int t, int j) {
+      const uint64_t qd = make_smem_desc(sbase + t * SM::q_tile, 16, 1024), kd = make_smem_desc(sbase + SM::k_off, 16, 1024);
+      const uint64_t vd = make_smem_desc(sbase + SM::v_off, 16384, 1024);
+      const uint32_t s_t = tmem + t * 128, o_t = tmem + 256 + t * D;
+      bool ok = nt == 0 || mbar_wait_warp<kIssueWaitHintNs>(bar_q, 0, abort_flag, a.status);
+      auto scores = [&](int j, int h) {                            // of the h-th kSub keys of tile j
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
-          umma_ss(tmem + t * 128, qd + ((t * SM::q_tile) >> 4) + off, kd + (((j % SK) * SM::q_tile) >> 4) + off, id_s, k != 0, lead);
+          umma_ss(s_t + 64 * h, qd + off, kd + (((j % SK) * SM::q_tile + h * 8192) >> 4) + off, id_s, k != 0, lead);
         }
-        umma_commit(bar_s + 8 * t, lead);
-        if (lead) mbar_arrive(bar_s + 8 * t);                      // what this warp has seen arrive (key scales) is there for those who wait
+        umma_commit(bar_s + 16 * t + 8 * h, lead);
+        if (lead) mbar_arrive(bar_s + 16 * t + 8 * h);             // what this warp has seen arrive (key scales) is there for those who wait
       };
-      if (ok) ok = mbar_wait_warp<kIssueWaitHintNs>(bar_k_full, 0, abort_flag, a.status);
-      if (ok) {
+      auto values = [&](int j, int h) {
+        const uint32_t p = kOver ? s_t + 64 * h : tmem + 384 + t * 64;
+#pragma unroll
+        for (int k = 0; k < kSub / 16; ++k) umma_ts(o_t, p + k * 8, vd + (((j % SV) * SM::q_tile + (4 * h + k) * 2048) >> 4), id_o, (j | h | k) != 0, lead);
+        umma_commit(bar_pv + 16 * t + 8 * h, lead);
+      };
+      auto leave = [&](uint32_t empty, bool used) {                // a stage that has been waited for
+        if (used) umma_commit(empty, lead);
+        else if (lead) mbar_arrive(empty);
+      };
+      auto have_k = [&](int j) {
+        const bool there = mbar_wait_warp<kIssueWaitHintNs>(bar_k_full + 8 * (j % SK), (j / SK) & 1, abort_flag, a.status);
         tc_fence_after();
-        for (int t = 0; t < 2; ++t)
-          if (it.nt[t] > 0) scores(t, 0);
-        umma_commit(bar_k_empty, lead);
+        return there;
+      };
+      if (ok && nt > 0) {
+        ok = have_k(0);
+        if (ok) {
+          if (n > 0) {
+            for (int h = 0; h < NS; ++h) scores(0, h);
+          }
+          leave(bar_k_empty, n > 0);
+        }
       }
       for (int j = 0; j < nt && ok; ++j) {
-        const int sk = (j + 1) % SK, sv = j % SV;
-        ok = mbar_wait_warp<kIssueWaitHintNs>(bar_v_full + 8 * sv, (j / SV) & 1, abort_flag, a.status);
-        if (!PAGED && j >= clean_from) ok = ok && mbar_wait_warp(bar_v_clean + 8 * sv, ((j - clean_from) / SV) & 1, abort_flag, a.status);
-        for (int t = 0; t < 2 && ok; ++t) {
-          if (j >= it.nt[t]) continue;
-          ok = mbar_wait_warp(bar_p + 8 * t, j & 1, abort_flag, a.status);
+        const bool mine = j < n, next = j + 1 < n;
+        for (int h = 0; h < NS && ok; ++h) {
+          auto next_scores = [&]() {                               // Q K^T of the same keys of the next tile
+            if (j + 1 >= nt) return;
+            if (h == 0) ok = ok && have_k(j + 1);
+            if (next && !kOver) ok = ok && mbar_wait_warp(bar_ld + 16 * t + 8 * h, j & 1, abort_flag, a.status);
+            if (!ok) return;
+            if (!kOver) tc_fence_after();
+            if (next) scores(j + 1, h);
+            if (h == NS - 1) leave(bar_k_empty + 8 * ((j + 1) % SK), next);
+          };
+          if (!kOver) next_scores();                               // beside the exponentials of this one
+          if (h == 0) {
+            ok = ok && mbar_wait_warp<kIssueWaitHintNs>(bar_v_full + 8 * (j % SV), (j / SV) & 1, abort_flag, a.status);
+            if (!PAGED && j >= clean_from) ok = ok && mbar_wait_warp(bar_v_clean + 8 * (j % SV), ((j - clean_from) / SV) & 1, abort_flag, a.status);
+          }
+          if (mine) ok = ok && mbar_wait_warp(bar_p + 16 * t + 8 * h, j & 1, abort_flag, a.status);
           if (!ok) break;
           tc_fence_after();
-#pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k)
-            umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, vd + ((sv * SM::q_tile + k * 2048) >> 4), id_o, (j | k) != 0, lead);
-          umma_commit(bar_pv + 8 * t, lead);
-          if (j + 1 < it.nt[t]) {
-            ok = mbar_wait_warp<kIssueWaitHintNs>(bar_k_full + 8 * sk, ((j + 1) / SK) & 1, abort_flag, a.status);
-            if (!ok) break;
-            tc_fence_after();
-            scores(t, j + 1);
-          }
+          if (mine) values(j, h);
+          if (kOver) next_scores();
         }
-        if (!ok) break;
-        if (j + 1 < nt) umma_commit(bar_k_empty + 8 * sk, lead);
-        umma_commit(bar_v_empty + 8 * sv, lead);
+        if (ok) leave(bar_v_empty + 8 * (j % SV), mine);
       }
-      umma_commit(bar_drain, lead);                                // nothing is in flight when tensor memory goes back
-      mbar_wait_warp(bar_drain, 0, done_flag, a.status);
+      umma_commit(bar_drain + 8 * t, lead);                        // nothing is in flight when tensor memory goes back
+      mbar_wait_warp(bar_drain + 8 * t, 0, done_flag, a.status);
     } else if (!PAGED && (warp == kKWarp || warp == kVWarp)) {
       // ================================================================ K or V tiles by TMA
       const bool is_k = warp == kKWarp;
@@ -245,7 +281,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       for (int j = max(0, copied - stages); j < copied; ++j) mbar_wait_warp(full + 8 * (j % stages), (j / stages) & 1, done_flag, a.status);      // all copies have landed
     }
   } else if (warp >= kMoveWarp) {
-    setmaxnreg_dec<kMoveRegs>();
+    set_regs<ManyRoles<D>::kMove>();
     const int tid = threadIdx.x - kMoveWarp * 32;
     // ================================================================ queries
     const T* q = static_cast<const T*>(a.q);
@@ -445,101 +481,121 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
     if (spoilt) *spoilt_s = 1;
   } else {
     // ================================================================== soft-max of query tile t, a thread a row
-    setmaxnreg_inc<kSoftmaxRegs>();
+    set_regs<ManyRoles<D>::kSoftmax>();
     const int t = warp >> 2, row = t * 128 + (threadIdx.x & 127), r = it.row0 + row, n = it.nt[t];
     const bool live = r < it.rows;
     const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
     const int end = live ? visible_end(it.past + i, s.len, a.frame) - it.k0 : 0;       // in the keys of the part
     const uint32_t lane_t = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_t = lane_t + t * 128, o_t = lane_t + 256 + t * D;
-    float f0 = rsqrtf(static_cast<float>(D)) * 1.4426950408889634f, f1 = f0, factor = f0;
+    float factor = rsqrtf(static_cast<float>(D)) * 1.4426950408889634f;
     if (PAGED && n > 0) {
       mbar_wait_warp(bar_q, 0, abort_flag, a.status);
       factor = reinterpret_cast<const float*>(smem + SM::factor_off)[row];
     }
     float m = -INFINITY;
-    float2 l = make_float2(0.f, 0.f);
+    float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      ok = ok && mbar_wait_warp(bar_s + 8 * t, j & 1, abort_flag, a.status);
+    for (int i2 = 0; i2 < NS * n; ++i2) {                          // the h-th kSub keys of tile j
+      const int j = i2 / NS, h = i2 % NS;
+      const uint32_t at = 16 * t + 8 * h;
+      ok = ok && mbar_wait_warp(bar_s + at, j & 1, abort_flag, a.status);
       if (!ok) break;
       tc_fence_after();
-      uint32_t x[4][32];
+      uint32_t x[kSub / 32][32];
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) tmem_ld32(s_t + q4 * 32, x[q4]);
+      for (int q = 0; q < kSub / 32; ++q) tmem_ld32(s_t + kSub * h + 32 * q, x[q]);
+      float f[2] = {factor, factor};                               // of the first and the second 64 keys of those
       if (PAGED) {
         float2 ks;
         asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks.x), "=f"(ks.y) : "r"(sbase + SM::scale_off + (j & 7) * 8));
-        f0 = factor * ks.x;
-        f1 = a.PT == 64 ? factor * ks.y : f0;
+        f[0] = factor * (a.PT == 64 && NS == 2 && h == 1 ? ks.y : ks.x);
+        f[1] = factor * (a.PT == 64 ? ks.y : ks.x);
       }
       tmem_wait_ld();
+      if (!kOver) {
+        tc_fence_before();
+        mbar_arrive_warp(bar_ld + at);
+      }
       if (j >= it.whole_from[t]) {
-        const int valid = end - j * kKeys;
+        const int valid = end - i2 * kSub;
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
+        for (int q = 0; q < kSub / 32; ++q)
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (q4 * 32 + e >= valid) x[q4][e] = 0xFF800000u;
+            if (q * 32 + e >= valid) x[q][e] = 0xFF800000u;
       }
-      float mx[4];
+      float top;
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        float v0 = fmax3(__uint_as_float(x[q4][0]), __uint_as_float(x[q4][1]), __uint_as_float(x[q4][2])), v1 = fmaxf(__uint_as_float(x[q4][3]), __uint_as_float(x[q4][4]));
+      for (int h2 = 0; h2 < kSub / 64; ++h2) {
+        float v[4];
 #pragma unroll
-        for (int e = 5; e < 29; e += 4) {
-          v0 = fmax3(v0, __uint_as_float(x[q4][e]), __uint_as_float(x[q4][e + 1]));
-          v1 = fmax3(v1, __uint_as_float(x[q4][e + 2]), __uint_as_float(x[q4][e + 3]));
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t* y = &x[2 * h2 + (q >> 1)][16 * (q & 1)];
+          v[q] = fmax3_nan(__uint_as_float(y[0]), __uint_as_float(y[1]), __uint_as_float(y[2]));
+#pragma unroll
+          for (int e = 3; e < 15; e += 2) v[q] = fmax3_nan(v[q], __uint_as_float(y[e]), __uint_as_float(y[e + 1]));
         }
-        mx[q4] = fmax3(fmax3(v0, __uint_as_float(x[q4][29]), __uint_as_float(x[q4][30])), v1, __uint_as_float(x[q4][31]));
+        v[0] = fmax3_nan(v[0], __uint_as_float(x[2 * h2][15]), __uint_as_float(x[2 * h2][31]));
+        v[1] = fmax3_nan(v[1], __uint_as_float(x[2 * h2 + 1][15]), __uint_as_float(x[2 * h2 + 1][31]));
+        const float w = fmax3_nan(fmax3_nan(v[0], v[1], v[2]), v[3], v[3]) * f[h2];
+        top = h2 ? fmax3_nan(top, w, w) : w;
       }
-      const float top = PAGED ? fmaxf(fmaxf(mx[0], mx[1]) * f0, fmaxf(mx[2], mx[3]) * f1) : fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * f0;
-      const bool raise = top > m + kRaise;                         // (at first m is -inf)
+      // P V of the same keys of the tile before is over: P lies where its probabilities were
+      if (!kOver && j > 0) {
+        ok = mbar_wait_warp(bar_pv + at, (j - 1) & 1, abort_flag, a.status);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const bool raise = !(top <= m + kRaise);                     // (at first m is -inf; a logit that is no number makes m, and with it all, none)
       if (__any_sync(0xffffffffu, raise)) {
-        const float to = raise ? top : m, alpha = raise ? (m == -INFINITY ? 0.f : fast_exp2(m - to)) : 1.f;
+        const float to = raise ? top : m, alpha = to == m ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - to);
         m = to;
-        l.x *= alpha;
-        l.y *= alpha;
-        if (j > 0) {
-          ok = mbar_wait_warp(bar_pv + 8 * t, (j - 1) & 1, abort_flag, a.status);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          l[q].x *= alpha;
+          l[q].y *= alpha;
+        }
+        if (i2 > 0) {                                              // O follows, once the keys before have been added to it
+          ok = mbar_wait_warp(bar_pv + 16 * t + 8 * ((i2 - 1) % NS), ((i2 - 1) / NS) & 1, abort_flag, a.status);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
-          for (int q4 = 0; q4 < D / 16; ++q4) {
-            uint32_t v[16];
-            tmem_ld16(o_t + q4 * 16, v);
+          for (int q = 0; q < D / 16; ++q) {
+            uint32_t y[16];
+            tmem_ld16(o_t + q * 16, y);
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
-            tmem_st16(o_t + q4 * 16, v);
+            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+            tmem_st16(o_t + q * 16, y);
           }
         }
       }
-      const float ref = m == -INFINITY ? 0.f : -m;
+      const float ref = fabsf(m) < INFINITY ? -m : m == -INFINITY ? 0.f : __int_as_float(0x7FC00000);
+      const float2 rr = make_float2(ref, ref);
 #pragma unroll
-      for (int q2 = 0; q2 < 2; ++q2) {
-        const float f = q2 ? f1 : f0;
-        const float2 ff = make_float2(f, f), rr = make_float2(ref, ref);
+      for (int h2 = 0; h2 < kSub / 64; ++h2) {
+        const float2 ff = make_float2(f[h2], f[h2]);
         uint32_t p[32];
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-          const uint32_t* v = &x[2 * q2 + (e >> 4)][2 * (e & 15)];
-          const float2 u = ffma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), ff, rr);
-          const float2 pr = make_float2(fast_exp2(u.x), fast_exp2(u.y));
+          const uint32_t* y = &x[2 * h2 + (e >> 4)][2 * (e & 15)];
+          const float2 u = ffma2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), ff, rr);
+          const float2 pr = e % 16 < kPoly ? poly_exp2(u) : make_float2(fast_exp2(u.x), fast_exp2(u.y));
           p[e] = narrow2<M>(pr.x, pr.y);
-          if (kHalf) add_f16x2(l, p[e]);
-          else add_bf16x2(l, p[e]);
+          if (kHalf) add_f16x2(l[e & 1], p[e]);
+          else add_bf16x2(l[e & 1], p[e]);
         }
-        tmem_st32(s_t + q2 * 32, p);
+        tmem_st32(kOver ? s_t + 64 * h : lane_t + 384 + t * 64 + 32 * h2, p);
       }
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive_warp(bar_p + 8 * t);
+      mbar_arrive_warp(bar_p + at);
     }
     // ---- the row's end
-    if (ok && n > 0) ok = mbar_wait_warp(bar_pv + 8 * t, (n - 1) & 1, abort_flag, a.status);
+    if (ok && n > 0) ok = mbar_wait_warp(bar_pv + 16 * t + 8 * (NS - 1), (n - 1) & 1, abort_flag, a.status);      // (in order: the other half is over too)
     tc_fence_after();
-    const float sum = l.x + l.y;
+    const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y);
     float unit = 1.f;
     if (PAGED && n > 0) unit = fmaxf(fmaxf(unit_s[0], unit_s[1]), fmaxf(unit_s[2], unit_s[3]));
     const int tok = s.t0 + i;
