@@ -34,9 +34,9 @@ struct DenseArgs {
   float* part_o;                   // [parts][T][H][D]
   float2* part_ml;                 // [parts][T][H]  reference (binary orders) and sum
   // few rows: items are cut where a CTA's share of all tiles ends (dense_few.cu)
-  int few_ctas;
-  float* few_o;                    // [2 few_ctas][few_rows][D]
-  float2* few_ml;                  // [2 few_ctas][few_rows]
+  int few_ctas, few_tile;          // rows of an item
+  float* few_o;                    // [2 few_ctas][few_tile][D]
+  float2* few_ml;                  // [2 few_ctas][few_tile]
   int2* few_pieces;                // [T][H]  place of the row's first piece, and the last CTA that has one (-1: the row is not cut)
 };
 
@@ -101,7 +101,7 @@ struct AppendArgs {
 };
 int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st);
 int launch_dense_many(const DenseArgs& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int D, bool fp16, cudaStream_t st);
-int few_rows_of(int64_t rows);
+int few_tile_of(int64_t rows, int D);
 int few_ctas_an_sm(int rows, int D);
 int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st);
 int launch_dense_join(const DenseArgs& a, int D, bool fp16, cudaStream_t st);

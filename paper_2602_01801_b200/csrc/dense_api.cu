@@ -67,7 +67,7 @@ int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int he
 
 // How attention over the cache is launched: which kernels, on how many CTAs, the parts of the kernel for many rows (of a multiple of 128 keys), and the workspace.
 struct AttendPlan {
-  int few_rows, few_ctas;          // 0: the kernel for few rows is not launched
+  int few_rows, few_ctas, few_tile;            // 0: the kernel for few rows is not launched
   bool many, join;
   int chunk, parts;
   size_t few_o, few_ml, few_pieces, part_o, part_ml, bytes;        // offsets
@@ -83,8 +83,10 @@ AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, in
   p.parts = 1;
   if (!p.many || !equal) {
     // as many CTAs as the SMs hold, or one for every 128 keys where there are fewer of those
-    p.few_rows = few_rows_of(rows);
-    const int64_t units = static_cast<int64_t>(B) * KV * ((len + kFewKeys - 1) / kFewKeys), most = few_ctas_an_sm(p.few_rows, D) * kSms;
+    p.few_rows = kFewRows;
+    p.few_tile = few_tile_of(rows, D);
+    const int64_t row_tiles = ((rows < kFewRows ? rows : kFewRows) + p.few_tile - 1) / p.few_tile;
+    const int64_t units = static_cast<int64_t>(B) * KV * row_tiles * ((len + kFewKeys - 1) / kFewKeys), most = few_ctas_an_sm(p.few_tile, D) * kSms;
     p.few_ctas = static_cast<int>(units < most ? units : most);
     p.join = len > kFewKeys;
   }
@@ -108,8 +110,8 @@ AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, in
   };
   p.bytes = 16;
   if (p.few_ctas > 0) {
-    p.few_o = take(static_cast<size_t>(2 * p.few_ctas) * p.few_rows * D * 4);
-    p.few_ml = take(static_cast<size_t>(2 * p.few_ctas) * p.few_rows * 8);
+    p.few_o = take(static_cast<size_t>(2 * p.few_ctas) * p.few_tile * D * 4);
+    p.few_ml = take(static_cast<size_t>(2 * p.few_ctas) * p.few_tile * 8);
     p.few_pieces = take(static_cast<size_t>(T) * H * 8);
   }
   if (p.parts > 1) {
@@ -198,7 +200,7 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   a.W = table_width; a.pages = num_pages; a.PT = page_tokens;
   const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim);
   uint8_t* w = static_cast<uint8_t*>(workspace);
-  a.few_rows = p.few_rows; a.few_ctas = p.few_ctas;
+  a.few_rows = p.few_rows; a.few_ctas = p.few_ctas; a.few_tile = p.few_tile;
   a.few_o = reinterpret_cast<float*>(w + p.few_o); a.few_ml = reinterpret_cast<float2*>(w + p.few_ml); a.few_pieces = reinterpret_cast<int2*>(w + p.few_pieces);
   a.parts = p.parts; a.chunk = p.chunk;
   a.part_o = reinterpret_cast<float*>(w + p.part_o); a.part_ml = reinterpret_cast<float2*>(w + p.part_ml);

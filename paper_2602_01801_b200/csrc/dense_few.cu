@@ -74,26 +74,28 @@ __device__ __forceinline__ uint32_t without_nan_codes(uint32_t v, bool& any) {
   return v & ~nan;
 }
 
-// The units (128 keys of a key head) of a sequence, sequences after one another, in a sequence key heads after one another.  CTA c of n takes the units
+// The units (128 keys of a key head, few_tile rows) of a sequence, sequences after one another, in a sequence key heads, in these row tiles.  CTA c of n takes the units
 // [U c / n, U (c + 1) / n): all have the same share, whatever the lengths are, and a CTA has two cut items at most, its first and its last.
 struct FewSeq {
   DenseSeq s;
-  int tiles;                                                       // of 128 keys
+  int tiles, row_tiles;                                            // of 128 keys, of few_tile rows
   int64_t units;
 };
 __device__ __forceinline__ int64_t few_seq(const DenseArgs& a, int b, FewSeq& f) {
   const int r = seq_of(a, b, f.s);
   if (r < 0 && a.status) record_status(a.status, kErrBounds);
-  f.tiles = f.s.n * a.G <= a.few_rows ? f.s.len / kFewKeys + (f.s.len % kFewKeys != 0 ? 1 : 0) : 0;
-  return f.units = static_cast<int64_t>(f.tiles) * a.KV;
+  const int rows = f.s.n * a.G;
+  f.row_tiles = rows <= a.few_rows ? (rows + a.few_tile - 1) / a.few_tile : 0;
+  f.tiles = f.s.len / kFewKeys + (f.s.len % kFewKeys != 0 ? 1 : 0);
+  return f.units = static_cast<int64_t>(f.tiles) * f.row_tiles * a.KV;
 }
 // A CTA's way through its pieces.
 struct FewWalk {
   int b;
   FewSeq f;
   int64_t base, x, x_end;                                          // units before the sequence; the next piece's first; the CTA's end
-  // the piece: key head, tiles [tile0, tile1) of the item, keys [k0, k1) of which some row sees all
-  int kvh, tile0, tile1, k0, k1;
+  // the piece: key head, row tile, tiles [tile0, tile1) of the item, keys [k0, k1) of which some row sees all
+  int kvh, rt, tile0, tile1, k0, k1;
   __device__ __forceinline__ bool next(const DenseArgs& a) {
     if (x >= x_end) return false;
     if (x - base == f.units) {                                     // the next sequence that has some
@@ -101,12 +103,15 @@ struct FewWalk {
       while (few_seq(a, ++b, f) == 0) {}
     }
     const int64_t at = x - base;
-    kvh = f.units <= INT32_MAX ? static_cast<int>(at) / f.tiles : static_cast<int>(at / f.tiles);
-    tile0 = static_cast<int>(at - static_cast<int64_t>(kvh) * f.tiles);
+    const int item = f.units <= INT32_MAX ? static_cast<int>(at) / f.tiles : static_cast<int>(at / f.tiles);
+    tile0 = static_cast<int>(at - static_cast<int64_t>(item) * f.tiles);
+    kvh = f.row_tiles == 1 ? item : item / f.row_tiles;
+    rt = item - kvh * f.row_tiles;
     tile1 = static_cast<int>(min(static_cast<int64_t>(f.tiles), tile0 + x_end - x));
     x += tile1 - tile0;
     k0 = tile0 * kFewKeys;
-    k1 = min(visible_end(f.s.len - 1, f.s.len, a.frame), tile1 == f.tiles ? f.s.len : tile1 * kFewKeys);
+    const int last = min(f.s.n * a.G, (rt + 1) * a.few_tile) - 1;
+    k1 = min(visible_end(f.s.len - f.s.n + last / a.G, f.s.len, a.frame), tile1 == f.tiles ? f.s.len : tile1 * kFewKeys);
     return true;
   }
 };
@@ -237,10 +242,10 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
     const int b = walk.b, kvh = walk.kvh, k0 = walk.k0, k1 = walk.k1;
     const bool whole = walk.tile0 == 0 && walk.tile1 == walk.f.tiles;
     const int place = (2 * blockIdx.x + (first_piece ? 0 : 1)) * R;            // where a cut item's piece goes
-    const int rows = s.n * a.G, past = s.len - s.n;
-    const int see_all = visible_end(past, s.len, a.frame);
+    const int row0 = walk.rt * R, rows = min(s.n * a.G - row0, R), past = s.len - s.n;      // this piece's first row, and how many it has
+    const int see_all = visible_end(past + row0 / a.G, s.len, a.frame);
     if (walk.tile0 == 0 && static_cast<int>(threadIdx.x) < rows) {
-      const int r = threadIdx.x, last = whole ? -1 : few_cta_of(units, walk.x - walk.tile1 + walk.f.tiles - 1, ctas);      // the CTA that has the item's last unit
+      const int r = row0 + threadIdx.x, last = whole ? -1 : few_cta_of(units, walk.x - walk.tile1 + walk.f.tiles - 1, ctas);      // the CTA that has the item's last unit
       a.few_pieces[static_cast<int64_t>(s.t0 + r / a.G) * a.H + kvh * a.G + r % a.G] = make_int2(place / R, last);
     }
 
@@ -250,9 +255,8 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
     int end[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      const int r = n * 8 + g;
-      const bool live = r < rows;
-      const int i = live ? r / a.G : 0, head = kvh * a.G + (live ? r - i * a.G : 0);
+      const bool live = n * 8 + g < rows;
+      const int r = live ? row0 + n * 8 + g : 0, i = r / a.G, head = kvh * a.G + r - i * a.G;
       const T* src = static_cast<const T*>(a.q) + head * a.q_hs + (s.t0 + i) * a.q_ts + c * (D / 4);
       uint4 v[D / 32];
       uint32_t most = 0;
@@ -282,7 +286,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
       for (int h = 0; h < 2; ++h) {
         factor[n][h] = __shfl_sync(0xffffffffu, up, (2 * c + h) * 4);
         const int r2 = n * 8 + 2 * c + h;
-        end[n][h] = r2 < rows ? visible_end(past + r2 / a.G, s.len, a.frame) : 0;
+        end[n][h] = r2 < rows ? visible_end(past + (row0 + r2) / a.G, s.len, a.frame) : 0;
       }
     }
 
@@ -423,7 +427,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
     if (__syncthreads_or(spoilt ? 1 : 0)) {
       // values that are no numbers where some row does not see them: straight from the definition
       for (int r = warp; r < rows; r += 4)
-        dense_row_to<T, D, true>(a, b, s.t0 + r / a.G, kvh * a.G + r % a.G, s, k0, k1, whole, a.few_o + static_cast<int64_t>(place + r) * D, a.few_ml + place + r);
+        dense_row_to<T, D, true>(a, b, s.t0 + (row0 + r) / a.G, kvh * a.G + (row0 + r) % a.G, s, k0, k1, whole, a.few_o + static_cast<int64_t>(place + r) * D, a.few_ml + place + r);
       continue;
     }
     // the warps' rows, with their units
@@ -457,7 +461,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
         f[w] = ml.x == -INFINITY && ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
         sum = fmaf(ml.y, f[w], sum);
       }
-      const int t = s.t0 + r / a.G, head = kvh * a.G + r % a.G;
+      const int t = s.t0 + (row0 + r) / a.G, head = kvh * a.G + (row0 + r) % a.G;
       const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       T* out = static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts;
 #pragma unroll
@@ -518,13 +522,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
     if (p.y < 0) return;
     first = p.x;
     parts = p.y - p.x / 2 + 1;
-    row_of_few = (t - s.t0) * a.G + head % a.G;
+    row_of_few = ((t - s.t0) * a.G + head % a.G) % a.few_tile;
   } else {
     if (a.parts == 1 || s.len <= a.chunk) return;
     parts = (s.len - 1) / a.chunk + 1;
   }
   auto place = [&](int p) {                                        // row of few_o, or of part_o
-    return few ? static_cast<int64_t>(p == 0 ? first : 2 * (first / 2 + p)) * a.few_rows + row_of_few : row + p * (static_cast<int64_t>(a.T) * a.H);
+    return few ? static_cast<int64_t>(p == 0 ? first : 2 * (first / 2 + p)) * a.few_tile + row_of_few : row + p * (static_cast<int64_t>(a.T) * a.H);
   };
   const float* from = few ? a.few_o : a.part_o;
   const float2* stat = few ? a.few_ml : a.part_ml;
@@ -588,8 +592,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
   store_cols<T, D>(static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts, lane, o, l == 0.f ? 0.f : 1.f / l);
 }
 
-// Rows that the kernel holds for a sequence of so many, 32 at most.
-int few_rows_of(int64_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+// Rows of an item where a sequence has so many at most.  32 rows of 128 columns do not fit the registers; two items of 16 read the keys twice, the second time
+// out of L2 (32 sequences of 24 tokens, 12 heads, 8 192 keys on average: 544 us as one item, with 700 bytes a thread spilled, 404 as two).
+int few_tile_of(int64_t rows, int D) { return rows <= 8 ? 8 : rows <= 16 || D == 128 ? 16 : 32; }
 
 template <class T, int D>
 static int launch_few_t(const DenseArgs& a, cudaStream_t st) {
@@ -599,13 +604,14 @@ static int launch_few_t(const DenseArgs& a, cudaStream_t st) {
     if (r != FASTAR_OK) return r;
     return launch_chained(few_kernel<T, D, NR>, a.few_ctas, kFewThreads, FewConf<D, NR>::total, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
   };
-  return a.few_rows == 8 ? go(std::integral_constant<int, 1>{}) : a.few_rows == 16 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+  if constexpr (D == 64) {
+    if (a.few_tile == 32) return go(std::integral_constant<int, 4>{});
+  }
+  return a.few_tile == 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
 }
-template <int D>
-static int few_ctas_t(int rows) {
-  return rows == 8 ? FewConf<D, 1>::CTAS : rows == 16 ? FewConf<D, 2>::CTAS : FewConf<D, 4>::CTAS;
+int few_ctas_an_sm(int tile, int D) {
+  return tile == 8 ? (D == 128 ? FewConf<128, 1>::CTAS : FewConf<64, 1>::CTAS) : tile == 16 ? (D == 128 ? FewConf<128, 2>::CTAS : FewConf<64, 2>::CTAS) : FewConf<64, 4>::CTAS;
 }
-int few_ctas_an_sm(int rows, int D) { return D == 128 ? few_ctas_t<128>(rows) : few_ctas_t<64>(rows); }
 
 int launch_dense_few(const DenseArgs& a, int D, bool fp16, cudaStream_t st) {
   if (fp16) return D == 128 ? launch_few_t<__half, 128>(a, st) : launch_few_t<__half, 64>(a, st);

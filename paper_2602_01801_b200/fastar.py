@@ -4,6 +4,7 @@ and streams.  There is no fallback: a missing library or a failing call raises."
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, Optional
 
@@ -441,6 +442,11 @@ def _dense_init():
     return _dense
 
 
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(*sizes) -> int:
+    return load_library().fastar_kv8_attention_workspace_bytes(*sizes)
+
+
 def _refuse(where: str):
     raise FastarError(ERR_INVALID_ARG, where)
 
@@ -481,7 +487,7 @@ def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add:
         with torch.cuda.device(dev):
             return block_tables(held, add, page_tokens, free_pages, first, table, max_add)
     B = held.shape[0]
-    cu, lens, first_out = torch.empty(2 * B + 2, dtype=i32, device=held.device).split((B + 1, B, 1))
+    cu, lens, first_out = torch.split_with_sizes(torch.empty(2 * B + 2, dtype=i32, device=held.device), (B + 1, B, 1))
     slots = torch.empty(max_add, dtype=torch.int64, device=held.device)
     _check(lib.fastar_block_tables(held.data_ptr(), add.data_ptr(), B, page_tokens, free_pages.data_ptr(), free_pages.shape[0], first.data_ptr(), table.data_ptr(),
                                    table.shape[1], cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), max_add, first_out.data_ptr(), _raw_stream(dev)), "fastar_block_tables")
@@ -521,7 +527,7 @@ def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_ne
         with torch.cuda.device(dev):
             return kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new, max_len, frame_len, out)
     out = _out_like(torch, q, strides, out, where)
-    nbytes = lib.fastar_kv8_attention_workspace_bytes(B, T, max_new, max_len, H, KV, D)
+    nbytes = _workspace_bytes(B, T, max_new, max_len, H, KV, D)
     work = torch.empty(nbytes, dtype=u8, device=q.device)
     _check(lib.fastar_kv8_attention(q.data_ptr(), out.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
                                     table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
