@@ -147,8 +147,13 @@ int launch_block_tables(const int32_t* held, const int32_t* add, int B, int PT, 
 // ---- append ------------------------------------------------------------------------------------------------------------------------------
 // codes = e4m3(x / s), s = 2^ceil(log2(amax / 448)) of the page's rows: with a power of two both the division and the product code x s are exact, and a
 // page whose scale grows is recoded exactly but for codes that fall below e4m3's least normal number.  A CTA takes the rows that go to one page of a
-// head: they stay in registers between the search for their largest value and the coding, so that every element is read once.
-constexpr int kAppendThreads = 128;
+// head, keys or values: they stay in registers (32 a thread) between the search for their largest value and the coding, so that every element is read once.
+// Where sequences bring a few tokens each, the way to the page is what takes time, and a warp does that for a head's keys or values.
+// (B200: 4 680 tokens of 12 heads of 128 11.8 us, 3.7 TB/s; 128 threads with 64 registers of rows each 12.1, 512 with 16 14.7.  One token each of 512 sequences,
+// 8 heads: a CTA each 67 us, a warp each 9.5.)
+constexpr int kAppendWarps = 8;                                    // of a CTA that has a warp for every head and tensor
+template <int D>
+constexpr int kAppendThreads = 2 * D;
 
 __device__ __forceinline__ uint32_t e4m3x4(float x0, float x1, float x2, float x3) {
   uint32_t r;
@@ -159,9 +164,51 @@ __device__ __forceinline__ float exp2i(int e) { return __uint_as_float(static_ca
 // Neither a number nor infinite values have a code of their own: both become the code that is no number.
 __device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) <= 3.4028235e38f ? x : __int_as_float(0x7FC00000); }
 
+__device__ __forceinline__ uint32_t largest(uint32_t most, float2 f) {
+  const uint32_t u = __float_as_uint(f.x) & 0x7FFFFFFFu, v = __float_as_uint(f.y) & 0x7FFFFFFFu;
+  return max(most, max(u < 0x7F800000u ? u : 0u, v < 0x7F800000u ? v : 0u));
+}
+// 16 elements as codes
+template <class T>
+__device__ __forceinline__ uint4 code16(const uint4& x0, const uint4& x1, float inv) {
+  uint4 o;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const uint4& x = h ? x1 : x0;
+      const float2 a = widen2<T>((&x.x)[2 * w]), b = widen2<T>((&x.x)[2 * w + 1]);
+      (&o.x)[2 * h + w] = e4m3x4(finite_or_nan(a.x * inv), finite_or_nan(a.y * inv), finite_or_nan(b.x * inv), finite_or_nan(b.y * inv));
+    }
+  return o;
+}
+// The page's other rows, from row `r0` on by `step`, at a scale larger by 1 / f
+template <int D>
+__device__ __forceinline__ void recode(uint8_t* page, int r0, int step, int page_rows, int row0, int rows, int c, float f) {
+  for (int r = r0; r < page_rows; r += step) {
+    if (r >= row0 && r < row0 + rows) continue;
+    uint4* at = reinterpret_cast<uint4*>(page + r * D + c * 16);
+    uint4 v = *at;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t& u = (&v.x)[w];
+      const float2 a = widen2<__half>(e4m3x2_to_half2(u & 0xFFFFu)), b = widen2<__half>(e4m3x2_to_half2(u >> 16));
+      u = e4m3x4(a.x * f, a.y * f, b.x * f, b.y * f);
+    }
+    *at = v;
+  }
+}
+
+struct AppendRun {                       // rows of the call that go to rows [row0, row0 + rows) of a page, which starts anew with the first
+  int64_t at, src;                       // page and head, first element
+  int rows, row0;
+};
 template <class T, int D>
-__device__ __forceinline__ void append_rows(const T* __restrict__ src, int64_t ts, int rows, int row0, int page_rows, bool fresh, uint8_t* page, float* scale, uint32_t* red) {
-  constexpr int TPR = D / 16, RPP = kAppendThreads / TPR, MAXP = 128 / RPP;      // threads a row, rows a pass
+__device__ __forceinline__ void append_rows(const AppendArgs& a, const AppendRun& w, bool v, uint32_t* red) {
+  constexpr int THREADS = kAppendThreads<D>, TPR = D / 16, RPP = THREADS / TPR, MAXP = 128 / RPP;      // threads a row, rows a pass
+  const T* src = static_cast<const T*>(v ? a.v : a.k) + w.src;
+  uint8_t* page = (v ? a.vc : a.kc) + w.at * a.PT * D;
+  float* scale = (v ? a.vs : a.ks) + w.at;
   const int c = threadIdx.x % TPR, r0 = threadIdx.x / TPR;
   uint4 x[MAXP][2];
   uint32_t most = 0;
@@ -169,67 +216,70 @@ __device__ __forceinline__ void append_rows(const T* __restrict__ src, int64_t t
   for (int p = 0; p < MAXP; ++p) {
     const int r = p * RPP + r0;
     x[p][0] = x[p][1] = make_uint4(0u, 0u, 0u, 0u);
-    if (r < rows) {
-      const uint4* at = reinterpret_cast<const uint4*>(src + r * ts + c * 16);
+    if (r < w.rows) {
+      const uint4* at = reinterpret_cast<const uint4*>(src + r * a.ts + c * 16);
       x[p][0] = __ldg(at);
       x[p][1] = __ldg(at + 1);
     }
   }
-  const float was = fresh ? 0.f : *scale;
+  const float was = w.row0 == 0 ? 0.f : *scale;
 #pragma unroll
   for (int p = 0; p < MAXP; ++p)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float2 f = widen2<T>((&x[p][h].x)[w]);
-        const uint32_t u = __float_as_uint(f.x) & 0x7FFFFFFFu, v = __float_as_uint(f.y) & 0x7FFFFFFFu;
-        most = max(most, max(u < 0x7F800000u ? u : 0u, v < 0x7F800000u ? v : 0u));
-      }
+    for (int e = 0; e < 8; ++e) most = largest(most, widen2<T>((&x[p][e >> 2].x)[e & 3]));
   most = __reduce_max_sync(0xffffffffu, most);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = most;
   __syncthreads();
-  most = max(max(red[0], red[1]), max(red[2], red[3]));
-  const float least = exp2i(scale_exp_of(most)), to = fmaxf(least, was);
-  const float inv = 1.f / to;            // a power of two (2^126 at most)
+#pragma unroll
+  for (int i = 0; i < THREADS / 32; ++i) most = max(most, red[i]);
+  const float to = fmaxf(exp2i(scale_exp_of(most)), was), inv = 1.f / to;        // a power of two (2^126 at most)
 #pragma unroll
   for (int p = 0; p < MAXP; ++p) {
     const int r = p * RPP + r0;
-    if (r >= rows) break;
-    uint32_t o[4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const float2 a = widen2<T>((&x[p][h].x)[2 * w]), b = widen2<T>((&x[p][h].x)[2 * w + 1]);
-        o[2 * h + w] = e4m3x4(finite_or_nan(a.x * inv), finite_or_nan(a.y * inv), finite_or_nan(b.x * inv), finite_or_nan(b.y * inv));
-      }
-    *reinterpret_cast<uint4*>(page + (row0 + r) * D + c * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (r >= w.rows) break;
+    *reinterpret_cast<uint4*>(page + (w.row0 + r) * D + c * 16) = code16<T>(x[p][0], x[p][1], inv);
   }
-  if (!fresh && was < to) {              // the page's other rows
-    const float f = was * inv;
-    for (int r = r0; r < page_rows; r += RPP) {
-      if (r >= row0 && r < row0 + rows) continue;
-      uint4* at = reinterpret_cast<uint4*>(page + r * D + c * 16);
-      uint4 v = *at;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t& u = (&v.x)[w];
-        const float2 a = widen2<__half>(e4m3x2_to_half2(u & 0xFFFFu)), b = widen2<__half>(e4m3x2_to_half2(u >> 16));
-        u = e4m3x4(a.x * f, a.y * f, b.x * f, b.y * f);
-      }
-      *at = v;
-    }
-  }
-  __syncthreads();                       // `scale` has been read, and `red`
+  if (w.row0 > 0 && was < to) recode<D>(page, r0, RPP, a.PT, w.row0, w.rows, c, was * inv);
+  // (every thread has read the scale before the barrier)
   if (threadIdx.x == 0 && was != to) *scale = to;
 }
-
+// The same by a warp, for any number of rows; those beyond the first pass are read twice.
 template <class T, int D>
-__global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const AppendArgs a) {
+__device__ __forceinline__ void append_rows_warp(const AppendArgs& a, const AppendRun& w, bool v) {
+  constexpr int TPR = D / 16, RPP = 32 / TPR;
+  const T* src = static_cast<const T*>(v ? a.v : a.k) + w.src;
+  uint8_t* page = (v ? a.vc : a.kc) + w.at * a.PT * D;
+  float* scale = (v ? a.vs : a.ks) + w.at;
+  const int lane = threadIdx.x & 31, c = lane % TPR, r0 = lane / TPR;
+  const float was = w.row0 == 0 ? 0.f : *scale;
+  uint32_t most = 0;
+  uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0;
+  auto read = [&](int r) {
+    const uint4* at = reinterpret_cast<const uint4*>(src + r * a.ts + c * 16);
+    x0 = __ldg(at);
+    x1 = __ldg(at + 1);
+  };
+  for (int r = r0 + (w.rows - 1 - r0) / RPP * RPP; r >= r0 && r0 < w.rows; r -= RPP) {      // the first pass last, to stay in registers
+    read(r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = largest(most, widen2<T>((&(e < 4 ? x0 : x1).x)[e & 3]));
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  const float to = fmaxf(exp2i(scale_exp_of(most)), was), inv = 1.f / to;
+  for (int r = r0; r < w.rows; r += RPP) {
+    if (r != r0) read(r);
+    *reinterpret_cast<uint4*>(page + (w.row0 + r) * D + c * 16) = code16<T>(x0, x1, inv);
+  }
+  if (w.row0 > 0 && was < to) recode<D>(page, r0, RPP, a.PT, w.row0, w.rows, c, was * inv);
+  if (lane == 0 && was != to) *scale = to;                         // (all lanes have read it: they met in the maximum)
+}
+
+// WARP: a warp for every head's keys and values, blockIdx.y counts eights of them; else a CTA for blockIdx.y's head, blockIdx.z its keys or values.
+template <class T, int D, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * kAppendWarps : kAppendThreads<D>) kv8_append_kernel(const AppendArgs a) {
   __shared__ int64_t red[66];
   __shared__ int found[2];
-  __shared__ uint32_t most[4];
+  __shared__ uint32_t most[kAppendThreads<D> / 32];
   chain_wait();
   chain_next();
   // the item-th touched page of the call
@@ -237,7 +287,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const Append
   const int64_t item = blockIdx.x;
   if (threadIdx.x == 0) found[0] = -1;
   __syncthreads();
-  for (int b0 = 0; b0 < a.B && before <= item; b0 += kAppendThreads) {
+  for (int b0 = 0; b0 < a.B && before <= item; b0 += blockDim.x) {
     const int b = b0 + threadIdx.x;
     int64_t n = 0, none = 0, all, all_none;
     int mine = 0;
@@ -259,26 +309,37 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const Append
   }
   const int b = found[0];
   if (b < 0) return;
-  const int t0 = a.cu[b], n = a.cu[b + 1] - t0, len = a.lens[b], past = len - n;
-  const int i = past / a.PT + found[1], kvh = blockIdx.y;
+  const int t0 = a.cu[b], n = a.cu[b + 1] - t0, len = a.lens[b], past = len - n, i = past / a.PT + found[1];
   const int page = a.table[static_cast<int64_t>(b) * a.W + i];
   if (page < 0 || page >= a.pages) {
     if (threadIdx.x == 0 && a.status) record_status(a.status, kErrBounds);
     return;
   }
-  const int lo = max(past, i * a.PT), rows = min(len - i * a.PT, a.PT) - (lo - i * a.PT), row0 = lo - i * a.PT;
-  const int64_t at = static_cast<int64_t>(page) * a.KV + kvh, src = kvh * a.hs + (t0 + lo - past) * a.ts;
-  const bool v = blockIdx.z != 0;
-  append_rows<T, D>(static_cast<const T*>(v ? a.v : a.k) + src, a.ts, rows, row0, a.PT, row0 == 0, (v ? a.vc : a.kc) + at * a.PT * D, (v ? a.vs : a.ks) + at, most);
+  const int job = blockIdx.y * kAppendWarps + (threadIdx.x >> 5), kvh = WARP ? job >> 1 : blockIdx.y;
+  if (kvh >= a.KV) return;                                         // (a warp of its own)
+  const int lo = max(past, i * a.PT);
+  AppendRun w;
+  w.row0 = lo - i * a.PT;
+  w.rows = min(len - i * a.PT, a.PT) - w.row0;
+  w.at = static_cast<int64_t>(page) * a.KV + kvh;
+  w.src = kvh * a.hs + (t0 + lo - past) * a.ts;
+  if constexpr (WARP) append_rows_warp<T, D>(a, w, (job & 1) != 0);
+  else append_rows<T, D>(a, w, blockIdx.z != 0, most);
 }
 
-int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st) {
+template <class T, int D>
+static int launch_append_t(const AppendArgs& a, cudaStream_t st) {
   // n tokens lie in no more pages than n, nor than (n - 2) / PT + 2
   const int64_t most = static_cast<int64_t>(a.T) / a.PT + 2 * static_cast<int64_t>(a.B), items = most < a.T ? most : a.T;
-  const dim3 grid(static_cast<unsigned>(items), a.KV, 2);
-  void (*kern)(AppendArgs) = fp16 ? (a.D == 128 ? kv8_append_kernel<__half, 128> : kv8_append_kernel<__half, 64>)
-                                  : (a.D == 128 ? kv8_append_kernel<__nv_bfloat16, 128> : kv8_append_kernel<__nv_bfloat16, 64>);
-  return launch_chained(kern, grid, kAppendThreads, 0, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+  const bool warp = a.T <= static_cast<int64_t>(a.B) * 8;
+  const dim3 grid(static_cast<unsigned>(items), warp ? (2 * a.KV + kAppendWarps - 1) / kAppendWarps : a.KV, warp ? 1 : 2);
+  return launch_chained(warp ? kv8_append_kernel<T, D, true> : kv8_append_kernel<T, D, false>, grid, warp ? 32 * kAppendWarps : kAppendThreads<D>, 0, st, a) == cudaSuccess
+             ? FASTAR_OK
+             : FASTAR_ERR_CUDA;
+}
+int launch_kv8_append(const AppendArgs& a, bool fp16, cudaStream_t st) {
+  if (fp16) return a.D == 128 ? launch_append_t<__half, 128>(a, st) : launch_append_t<__half, 64>(a, st);
+  return a.D == 128 ? launch_append_t<__nv_bfloat16, 128>(a, st) : launch_append_t<__nv_bfloat16, 64>(a, st);
 }
 
 }  // namespace fastar
