@@ -40,9 +40,9 @@ int dense_device(int32_t** status) {
 }
 
 bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-// Rows of `heads` heads: 16-byte pieces, not overlapping
-bool rows_ok(const void* p, int64_t hs, int64_t ts, int heads, int d) {
-  return p && aligned(p, 16) && hs >= 0 && ts >= d && hs % 8 == 0 && ts % 8 == 0 && (heads == 1 || hs >= d);
+// Rows of `heads` heads: 16-byte pieces, not overlapping (a stride over one head or one token is not used)
+bool rows_ok(const void* p, int64_t hs, int64_t ts, int heads, int tokens, int d) {
+  return p && aligned(p, 16) && (tokens == 1 || (ts >= d && ts % 8 == 0)) && (heads == 1 || (hs >= d && hs % 8 == 0));
 }
 int shape_ok(int H, int KV, int D, int dtype) {
   if (KV < 1 || H < KV || H % KV != 0) return FASTAR_ERR_INVALID_ARG;
@@ -51,13 +51,15 @@ int shape_ok(int H, int KV, int D, int dtype) {
   if (H > 65535) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   return FASTAR_OK;
 }
-// Rows of a key head and positions are counted in 32 bits.
+// Rows and positions are counted in 32 bits.
 constexpr int64_t kMostRows = int64_t{1} << 30;
-bool too_long(int total, int max_len, int H, int KV) { return static_cast<int64_t>(total) * (H / KV) > kMostRows || max_len > kMostRows; }
+bool too_long(int total, int max_len, int H) { return static_cast<int64_t>(total) * H > kMostRows || max_len > kMostRows; }
 // Tiles of 128 tokens x 64 columns of a packed tensor [heads][T][d].
 int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int heads, int64_t ts, int64_t hs, bool fp16) {
+  if (tokens == 1) ts = d;                                         // (a stride over one token or one head is not used)
+  if (heads == 1) hs = ts;
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(tokens), static_cast<cuuint64_t>(heads)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ts) * 2, static_cast<cuuint64_t>(heads == 1 ? ts : hs) * 2};      // (one head: its stride is not used)
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ts) * 2, static_cast<cuuint64_t>(hs) * 2};
   const cuuint32_t box[3] = {64, 128, 1}, estr[3] = {1, 1, 1};
   return g_dense_encode(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
@@ -153,8 +155,9 @@ extern "C" int fastar_kv8_append(const void* k_new, const void* v_new, int64_t h
     return FASTAR_ERR_INVALID_ARG;
   if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
   if (total_tokens == 0) return FASTAR_OK;
-  if (!rows_ok(k_new, head_stride, token_stride, num_kv_heads, head_dim) || !rows_ok(v_new, head_stride, token_stride, num_kv_heads, head_dim))
+  if (!rows_ok(k_new, head_stride, token_stride, num_kv_heads, total_tokens, head_dim) || !rows_ok(v_new, head_stride, token_stride, num_kv_heads, total_tokens, head_dim))
     return FASTAR_ERR_INVALID_ARG;
+  if (too_long(total_tokens, 1, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   AppendArgs a{};
   a.k = k_new; a.v = v_new; a.hs = head_stride; a.ts = token_stride;
   a.T = total_tokens; a.B = num_seqs; a.KV = num_kv_heads; a.D = head_dim; a.PT = page_tokens; a.W = table_width; a.pages = num_pages;
@@ -168,7 +171,7 @@ extern "C" int fastar_kv8_append(const void* k_new, const void* v_new, int64_t h
 extern "C" size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
                                                        int32_t num_kv_heads, int32_t head_dim) {
   if (shape_ok(num_heads, num_kv_heads, head_dim, FASTAR_BF16) != FASTAR_OK || num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new ||
-      too_long(total_tokens, max_len, num_heads, num_kv_heads))
+      too_long(total_tokens, max_len, num_heads))
     return 0;
   return attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim).bytes;
 }
@@ -183,7 +186,7 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   if (num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new || frame_len < 0 || num_pages < 1 || table_width < 1) return FASTAR_ERR_INVALID_ARG;
   if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (max_len > static_cast<int64_t>(table_width) * page_tokens) return FASTAR_ERR_INVALID_ARG;
-  if (too_long(total_tokens, max_len, num_heads, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (too_long(total_tokens, max_len, num_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (!table || !lens || !cu || !aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
   if (!k_codes || !v_codes || !k_scale || !v_scale || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
     return FASTAR_ERR_INVALID_ARG;
@@ -191,7 +194,8 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
       workspace_bytes < fastar_kv8_attention_workspace_bytes(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim))
     return FASTAR_ERR_WORKSPACE;
   if (total_tokens == 0) return FASTAR_OK;
-  if (!rows_ok(q, head_stride, token_stride, num_heads, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, head_dim)) return FASTAR_ERR_INVALID_ARG;
+  if (!rows_ok(q, head_stride, token_stride, num_heads, total_tokens, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, total_tokens, head_dim) || q == out)
+    return FASTAR_ERR_INVALID_ARG;
   DenseArgs a{};
   a.q = q; a.out = out; a.q_hs = head_stride; a.q_ts = token_stride;
   a.T = total_tokens; a.B = num_seqs; a.H = num_heads; a.KV = num_kv_heads; a.G = num_heads / num_kv_heads;
@@ -221,10 +225,12 @@ extern "C" int fastar_packed_attention(const void* q, const void* k, const void*
   int r = shape_ok(num_heads, num_kv_heads, head_dim, dtype);
   if (r != FASTAR_OK) return r;
   if (num_seqs < 1 || total_tokens < 0 || max_tokens < 1 || frame_len < 0 || !cu || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
-  if (too_long(total_tokens, max_tokens, num_heads, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (too_long(total_tokens, max_tokens, num_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (total_tokens == 0) return FASTAR_OK;
-  if (!rows_ok(q, head_stride, token_stride, num_heads, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, head_dim)) return FASTAR_ERR_INVALID_ARG;
-  if (!rows_ok(k, kv_head_stride, kv_token_stride, num_kv_heads, head_dim) || !rows_ok(v, kv_head_stride, kv_token_stride, num_kv_heads, head_dim))
+  if (!rows_ok(q, head_stride, token_stride, num_heads, total_tokens, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, total_tokens, head_dim) || q == out)
+    return FASTAR_ERR_INVALID_ARG;
+  if (!rows_ok(k, kv_head_stride, kv_token_stride, num_kv_heads, total_tokens, head_dim) || !rows_ok(v, kv_head_stride, kv_token_stride, num_kv_heads, total_tokens, head_dim) ||
+      k == out || v == out)
     return FASTAR_ERR_INVALID_ARG;
   DenseArgs a{};
   a.q = q; a.out = out; a.q_hs = head_stride; a.q_ts = token_stride;

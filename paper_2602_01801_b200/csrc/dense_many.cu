@@ -307,7 +307,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
         uint32_t most = 0;
 #pragma unroll 4
         for (int p = 0; p < D / 8; ++p) {
-          const uint4 v = live ? __ldg(src + p) : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 v = live ? __ldcg(src + p) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 f = widen2<T>((&v.x)[e]);
@@ -320,7 +320,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
         factor[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (rsqrtf(static_cast<float>(D)) * 1.4426950408889634f);
 #pragma unroll 4
         for (int p = 0; p < D / 8; ++p) {
-          uint4 v = live ? __ldg(src + p) : make_uint4(0u, 0u, 0u, 0u);
+          uint4 v = live ? __ldcg(src + p) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const float2 f = widen2<T>((&v.x)[w]);
@@ -414,7 +414,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       };
       auto ask = [&](const Unit& w, int p) {                       // RPP rows x D codes are 2048 bytes
         const uint8_t* at = (p < PASSES / 2 ? w.at0 : w.at1) + p * 2048;
-        return w.there && p * RPP + r0 < w.left ? __ldg(reinterpret_cast<const uint4*>(at)) : make_uint4(0u, 0u, 0u, 0u);
+        return w.there && p * RPP + r0 < w.left ? __ldcg(reinterpret_cast<const uint4*>(at)) : make_uint4(0u, 0u, 0u, 0u);
       };
       auto convert = [&](const Unit& w, uint4 (&raw)[PASSES], const Unit& next) {
         if (!w.there) return true;                                 // (K(nt) only: behind it there is V(nt - 1), which has been asked for)

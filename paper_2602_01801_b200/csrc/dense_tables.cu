@@ -47,8 +47,7 @@ struct TableReq {
 };
 
 __global__ void __launch_bounds__(kTableThreads)
-block_tables_kernel(const int32_t* __restrict__ held, const int32_t* __restrict__ add, int B, int PT, const int32_t* __restrict__ free_pages, int n_free,
-                    const int32_t* __restrict__ first, int32_t* table, int W, int32_t* __restrict__ cu, int32_t* __restrict__ lens, int64_t* __restrict__ slots,
+block_tables_kernel(const int32_t* held, const int32_t* add, int B, int PT, const int32_t* free_pages, int n_free, const int32_t* first, int32_t* table, int W, int32_t* __restrict__ cu, int32_t* __restrict__ lens, int64_t* __restrict__ slots,
                     int max_add, int32_t* __restrict__ first_out, int32_t* status) {
   __shared__ TableReq req[kTableThreads + 1];
   __shared__ int64_t red[66];
@@ -218,8 +217,8 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const AppendRun
     x[p][0] = x[p][1] = make_uint4(0u, 0u, 0u, 0u);
     if (r < w.rows) {
       const uint4* at = reinterpret_cast<const uint4*>(src + r * a.ts + c * 16);
-      x[p][0] = __ldg(at);
-      x[p][1] = __ldg(at + 1);
+      x[p][0] = __ldcg(at);
+      x[p][1] = __ldcg(at + 1);
     }
   }
   const float was = w.row0 == 0 ? 0.f : *scale;
@@ -256,8 +255,8 @@ __device__ __forceinline__ void append_rows_warp(const AppendArgs& a, const Appe
   uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0;
   auto read = [&](int r) {
     const uint4* at = reinterpret_cast<const uint4*>(src + r * a.ts + c * 16);
-    x0 = __ldg(at);
-    x1 = __ldg(at + 1);
+    x0 = __ldcg(at);
+    x1 = __ldcg(at + 1);
   };
   for (int r = r0 + (w.rows - 1 - r0) / RPP * RPP; r >= r0 && r0 < w.rows; r -= RPP) {      // the first pass last, to stay in registers
     read(r);

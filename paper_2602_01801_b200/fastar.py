@@ -480,7 +480,8 @@ def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add:
     entries are written in place.  Returns cu [B+1], lens [B] (-1: refused), slots [max_add] int64 and first [1], where the free list goes on."""
     lib, torch, _, i32, _, _, current = _dense or _dense_init()
     where, dev = "block_tables", held.get_device()
-    if not (dev >= 0 and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and first.numel() == 1 and max_add >= 0
+    if not (dev >= 0 and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and free_pages.dim() == 1
+            and first.numel() == 1 and max_add >= 0
             and _ints_ok(i32, dev, held, add, free_pages, first, table)):
         _refuse(where)
     if dev != current():

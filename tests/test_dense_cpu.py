@@ -25,13 +25,13 @@ BIG = 1 << 20
 
 
 def packed_args(p, **kw):
-    a = dict(q=p, k=p, v=p, out=p, hs=BIG, ts=128, khs=BIG, kts=128, cu=p, seqs=2, total=10, max=5, H=4, KV=2, D=128, dtype=0, frame=1, stream=None)
+    a = dict(q=p, k=p, v=p, out=p + 2048, hs=BIG, ts=128, khs=BIG, kts=128, cu=p, seqs=2, total=10, max=5, H=4, KV=2, D=128, dtype=0, frame=1, stream=None)
     a.update(kw)
     return list(a.values())
 
 
 def attend_args(p, **kw):
-    a = dict(q=p, out=p, hs=BIG, ts=128, kc=p, vc=p, ks=p, vs=p, pages=4, PT=64, table=p, W=4, lens=p, cu=p, seqs=2, total=10, max_new=5, max_len=256, H=4, KV=2, D=128,
+    a = dict(q=p, out=p + 2048, hs=BIG, ts=128, kc=p, vc=p, ks=p, vs=p, pages=4, PT=64, table=p, W=4, lens=p, cu=p, seqs=2, total=10, max_new=5, max_len=256, H=4, KV=2, D=128,
              dtype=0, frame=1, work=p, bytes=1 << 40, stream=None)
     a.update(kw)
     return list(a.values())
@@ -52,12 +52,14 @@ def table_args(p, **kw):
 @pytest.mark.parametrize("bad,status", [
     (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(out=None), -1), (dict(cu=None), -1), (dict(seqs=0), -1), (dict(total=-1), -1), (dict(max=0), -1),
     (dict(H=3), -1), (dict(KV=0), -1), (dict(H=1), -1), (dict(D=96), -2), (dict(dtype=1), -1), (dict(dtype=3), -1), (dict(frame=-1), -1), (dict(ts=64), -1),
-    (dict(kts=120), -1), (dict(hs=100), -1), (dict(max=2 ** 30 + 1), -2), (dict(total=2 ** 30), -2), (dict(ts=132), -1), (dict(khs=0), -1), (dict(hs=-BIG), -1)])
+    (dict(kts=120), -1), (dict(hs=100), -1), (dict(max=2 ** 30 + 1), -2), (dict(total=2 ** 29), -2), (dict(ts=132), -1), (dict(khs=0), -1), (dict(hs=-BIG), -1)])
 def test_packed_refusals(lib, mem, bad, status):
     assert lib.fastar_packed_attention(*packed_args(mem[0], **bad)) == status
     if "q" in bad:
         assert lib.fastar_packed_attention(*packed_args(mem[0], q=mem[0] + 2)) == -1
         assert lib.fastar_packed_attention(*packed_args(mem[0], cu=mem[0] + 2)) == -1
+        for name in ("q", "k", "v"):                                            # in place
+            assert lib.fastar_packed_attention(*packed_args(mem[0], **{name: mem[0] + 2048})) == -1
 
 
 @pytest.mark.parametrize("bad,status", [
@@ -69,6 +71,7 @@ def test_paged_refusals(lib, mem, bad, status):
     if "q" in bad:
         assert lib.fastar_kv8_attention(*attend_args(mem[0], kc=mem[0] + 8)) == -1
         assert lib.fastar_kv8_attention(*attend_args(mem[0], work=mem[0] + 8)) == -7
+        assert lib.fastar_kv8_attention(*attend_args(mem[0], out=mem[0])) == -1             # in place
 
 
 @pytest.mark.parametrize("bad,status", [

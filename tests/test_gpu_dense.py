@@ -620,6 +620,21 @@ def test_two_captured_calls_at_once(fastar):
         assert torch.equal(o, w)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_strides_that_are_not_used(fastar, D):
+    """One token, or one head: whatever the stride over it says."""
+    g = gen(15)
+    x = rows(g, 1, 6, D, torch.bfloat16)
+    one = [t.as_strided((2, 1, D), (D, 3, 1)) for t in (rows(g, 2, 1, D, torch.bfloat16) for _ in range(3))]
+    head = [t.as_strided((1, 6, D), (5, D, 1)) for t in (x, rows(g, 1, 6, D, torch.bfloat16), rows(g, 1, 6, D, torch.bfloat16))]
+    for q, k, v in (one, head):
+        T = q.shape[1]
+        out = torch.empty_like(q.contiguous()).as_strided(q.shape, q.stride())
+        got = fastar.packed_attention(q, k, v, i32([0, T]), T, out=out)
+        want = fastar.packed_attention(*(t.clone(memory_format=torch.contiguous_format) for t in (q, k, v)), i32([0, T]), T)
+        assert torch.equal(got, want)
+
+
 def test_on_another_stream(fastar):
     g = gen(14)
     q, k, v = (rows(g, 2, 700, 64, torch.bfloat16) for _ in range(3))
