@@ -421,8 +421,8 @@ int fastar_kv8_append(const void* k_new, const void* v_new, int64_t head_stride,
 
 /* Attention of the new tokens (q, out: dev [num_heads][T][d], same strides) over the cache, their own keys included (append first).
  * One token a sequence, a few, or thousands; sequences of all lengths in one call.  workspace: dev, 16-byte aligned, of at least
- * fastar_kv8_attention_workspace_bytes (0 on invalid arguments; else 16 or more), contents irrelevant before and after; it
- * belongs to one call at a time. */
+ * fastar_kv8_attention_workspace_bytes (0 on invalid arguments; else 16 or more; with 16 none is used, and it may be null), contents
+ * irrelevant before and after; it belongs to one call at a time. */
 size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
                                             int32_t num_kv_heads, int32_t head_dim);
 int fastar_kv8_attention(const void* q, void* out, int64_t head_stride, int64_t token_stride, const uint8_t* k_codes, const uint8_t* v_codes,

@@ -34,7 +34,8 @@ struct DenseArgs {
   float* part_o;                   // [parts][T][H][D]
   float2* part_ml;                 // [parts][T][H]  reference (binary orders) and sum
   // few rows: items are cut where a CTA's share of all tiles ends (dense_few.cu)
-  int few_ctas, few_tile;          // rows of an item
+  int few_ctas, few_tile, few_row_tiles;       // rows of an item, most items of a sequence and key head
+  int cta_share;                   // CTAs of an item, a cluster, which takes all of it; 0: items are cut as above
   float* few_o;                    // [2 few_ctas][few_tile][D]
   float2* few_ml;                  // [2 few_ctas][few_tile]
   int2* few_pieces;                // [T][H]  place of the row's first piece, and the last CTA that has one (-1: the row is not cut)

@@ -69,7 +69,7 @@ int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int he
 
 // How attention over the cache is launched: which kernels, on how many CTAs, the parts of the kernel for many rows (of a multiple of 128 keys), and the workspace.
 struct AttendPlan {
-  int few_rows, few_ctas, few_tile;            // 0: the kernel for few rows is not launched
+  int few_rows, few_ctas, few_tile, few_row_tiles, cta_share;      // 0: the kernel for few rows is not launched; its items are cut
   bool many, join;
   int chunk, parts;
   size_t few_o, few_ml, few_pieces, part_o, part_ml, bytes;        // offsets
@@ -87,10 +87,18 @@ AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, in
     // as many CTAs as the SMs hold, or one for every 128 keys where there are fewer of those
     p.few_rows = kFewRows;
     p.few_tile = few_tile_of(rows, D);
-    const int64_t row_tiles = ((rows < kFewRows ? rows : kFewRows) + p.few_tile - 1) / p.few_tile;
-    const int64_t units = static_cast<int64_t>(B) * KV * row_tiles * ((len + kFewKeys - 1) / kFewKeys), most = few_ctas_an_sm(p.few_tile, D) * kSms;
+    p.few_row_tiles = static_cast<int>(((rows < kFewRows ? rows : kFewRows) + p.few_tile - 1) / p.few_tile);
+    const int64_t items = static_cast<int64_t>(B) * KV * p.few_row_tiles, units = items * tiles, most = few_ctas_an_sm(p.few_tile, D) * kSms;
     p.few_ctas = static_cast<int>(units < most ? units : most);
-    p.join = len > kFewKeys;
+    p.join = tiles > 1;
+    // A cluster an item, where none has more than four tiles a CTA and all are on the SMs at once
+    int share = 8;
+    while (share > 1 && share > tiles) share /= 2;
+    if (items * share <= most && tiles <= 4 * share) {
+      p.cta_share = share;
+      p.few_ctas = static_cast<int>(items * share);
+      p.join = false;
+    }
   }
   if (p.many) {
     // One CTA an SM: the parts that take the fewest rounds x (key tiles + 3, what a CTA takes to begin and end), with three more for the join
@@ -111,7 +119,7 @@ AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, in
     return at;
   };
   p.bytes = 16;
-  if (p.few_ctas > 0) {
+  if (p.few_ctas > 0 && p.cta_share == 0) {
     p.few_o = take(static_cast<size_t>(2 * p.few_ctas) * p.few_tile * D * 4);
     p.few_ml = take(static_cast<size_t>(2 * p.few_ctas) * p.few_tile * 8);
     p.few_pieces = take(static_cast<size_t>(T) * H * 8);
@@ -190,9 +198,8 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   if (!table || !lens || !cu || !aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
   if (!k_codes || !v_codes || !k_scale || !v_scale || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
     return FASTAR_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 16) ||
-      workspace_bytes < fastar_kv8_attention_workspace_bytes(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim))
-    return FASTAR_ERR_WORKSPACE;
+  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim);
+  if (p.bytes > 16 && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.bytes)) return FASTAR_ERR_WORKSPACE;
   if (total_tokens == 0) return FASTAR_OK;
   if (!rows_ok(q, head_stride, token_stride, num_heads, total_tokens, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, total_tokens, head_dim) || q == out)
     return FASTAR_ERR_INVALID_ARG;
@@ -202,9 +209,8 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   a.cu = cu; a.frame = frame_len; a.max_new = max_new; a.max_len = max_len;
   a.kc = k_codes; a.vc = v_codes; a.ks = k_scale; a.vs = v_scale; a.table = table; a.lens = lens;
   a.W = table_width; a.pages = num_pages; a.PT = page_tokens;
-  const AttendPlan p = attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim);
   uint8_t* w = static_cast<uint8_t*>(workspace);
-  a.few_rows = p.few_rows; a.few_ctas = p.few_ctas; a.few_tile = p.few_tile;
+  a.few_rows = p.few_rows; a.few_ctas = p.few_ctas; a.few_tile = p.few_tile; a.few_row_tiles = p.few_row_tiles; a.cta_share = p.cta_share;
   a.few_o = reinterpret_cast<float*>(w + p.few_o); a.few_ml = reinterpret_cast<float2*>(w + p.few_ml); a.few_pieces = reinterpret_cast<int2*>(w + p.few_pieces);
   a.parts = p.parts; a.chunk = p.chunk;
   a.part_o = reinterpret_cast<float*>(w + p.part_o); a.part_ml = reinterpret_cast<float2*>(w + p.part_ml);

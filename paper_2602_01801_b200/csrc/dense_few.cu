@@ -34,7 +34,8 @@ struct FewConf {
   static constexpr int pitch = D + 4;                              // floats of a row in the join of the warps
   static constexpr int join = scales + 4 * STAGES * 8;
   static constexpr int stat = join + 4 * 8 * NR * pitch * 4;       // [4][8 NR] (m, l) behind the rows
-  static constexpr int total = stat + 4 * 8 * NR * 8;
+  static constexpr int sums = stat + 4 * 8 * NR * 8;               // [8 NR] of the CTA, its rows where the first warp's were
+  static constexpr int total = sums + 8 * NR * 8;
 };
 
 // Where a 16-byte piece of a row lies: eight rows' same piece, and a row pair's neighbouring ones, fall into different banks.
@@ -118,7 +119,28 @@ struct FewWalk {
 __device__ __forceinline__ int64_t few_first(int64_t units, int c, int n) { return units * c / n; }
 __device__ __forceinline__ int few_cta_of(int64_t units, int64_t x, int n) { return static_cast<int>(((x + 1) * n - 1) / units); }
 
-template <class T, int D, int NR>
+// Clusters: where all items' shares fit the SMs at once, `cta_share` CTAs (1, 2, 4 or 8, a cluster) take equal parts of an item's keys and add them up out of each
+// other's shared memory, which spares the way through memory, the join's launch, and the sum over all sequences.  (SMALL)
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t shared, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(shared), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float4 ld_rank4(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_rank2(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+
+template <class T, int D, int NR, bool SMALL>
 __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(const DenseArgs a) {
   using SM = FewConf<D, NR>;
   constexpr int TILE = SM::TILE, STAGES = SM::STAGES, MT = TILE / 16, R = 8 * NR;
@@ -129,7 +151,22 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
   const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   chain_wait();
   chain_next();
-  {
+  FewWalk walk, asked;
+  int64_t units = 0;
+  int ctas = 0;
+  if constexpr (SMALL) {
+    const int share = a.cta_share, id = blockIdx.x / share, rank = blockIdx.x % share, of_seq = a.KV * a.few_row_tiles;
+    walk.b = id / of_seq;
+    few_seq(a, walk.b, walk.f);
+    walk.kvh = (id % of_seq) / a.few_row_tiles;
+    walk.rt = id % a.few_row_tiles;
+    if (walk.rt >= walk.f.row_tiles || walk.f.tiles == 0) return;  // (the whole cluster)
+    const int64_t item = (static_cast<int64_t>(walk.kvh) * walk.f.row_tiles + walk.rt) * walk.f.tiles;
+    walk.base = 0;
+    walk.x = item + static_cast<int64_t>(walk.f.tiles) * rank / share;
+    walk.x_end = item + static_cast<int64_t>(walk.f.tiles) * (rank + 1) / share;
+  } else {
+    {
     int64_t* red = reinterpret_cast<int64_t*>(smem);
     FewSeq f;
     auto scan = [&](int b, int64_t& mine, int64_t& step) {         // units before sequence b of this step's, b's and the step's
@@ -174,15 +211,15 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
       if (base > first) break;
     }
     __syncthreads();
+    }
+    units = found_s[0];
+    ctas = units < gridDim.x ? static_cast<int>(units) : gridDim.x;
+    walk.b = static_cast<int>(found_s[2]);
+    walk.base = found_s[1];
+    walk.x = few_first(units, blockIdx.x, ctas);
+    walk.x_end = few_first(units, blockIdx.x + 1, ctas);
+    few_seq(a, walk.b, walk.f);
   }
-  const int64_t units = found_s[0];
-  const int ctas = units < gridDim.x ? static_cast<int>(units) : gridDim.x;
-  FewWalk walk, asked;
-  walk.b = static_cast<int>(found_s[2]);
-  walk.base = found_s[1];
-  walk.x = few_first(units, blockIdx.x, ctas);
-  walk.x_end = few_first(units, blockIdx.x + 1, ctas);
-  few_seq(a, walk.b, walk.f);
   asked = walk;
 
   // ---- copies: a warp's tiles of all pieces, one after the other
@@ -237,14 +274,16 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
   for (int i = 0; i < STAGES - 1; ++i) ask();
   uint32_t st = 0;
 
+  if (SMALL && walk.x == walk.x_end)                               // more CTAs than tiles: nothing to add to the cluster's sums
+    for (int r = threadIdx.x; r < R; r += kFewThreads) *reinterpret_cast<float2*>(smem + SM::sums + r * 8) = make_float2(-INFINITY, 0.f);
   for (bool first_piece = true; walk.next(a); first_piece = false) {
     const DenseSeq s = walk.f.s;
     const int b = walk.b, kvh = walk.kvh, k0 = walk.k0, k1 = walk.k1;
-    const bool whole = walk.tile0 == 0 && walk.tile1 == walk.f.tiles;
+    const bool whole = SMALL ? a.cta_share == 1 : walk.tile0 == 0 && walk.tile1 == walk.f.tiles;
     const int place = (2 * blockIdx.x + (first_piece ? 0 : 1)) * R;            // where a cut item's piece goes
     const int row0 = walk.rt * R, rows = min(s.n * a.G - row0, R), past = s.len - s.n;      // this piece's first row, and how many it has
     const int see_all = visible_end(past + row0 / a.G, s.len, a.frame);
-    if (walk.tile0 == 0 && static_cast<int>(threadIdx.x) < rows) {
+    if (!SMALL && walk.tile0 == 0 && static_cast<int>(threadIdx.x) < rows) {
       const int r = row0 + threadIdx.x, last = whole ? -1 : few_cta_of(units, walk.x - walk.tile1 + walk.f.tiles - 1, ctas);      // the CTA that has the item's last unit
       a.few_pieces[static_cast<int64_t>(s.t0 + r / a.G) * a.H + kvh * a.G + r % a.G] = make_int2(place / R, last);
     }
@@ -424,15 +463,17 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
       __syncwarp();                                                // the stage may be filled again
     }
 
+    float* join = reinterpret_cast<float*>(smem + SM::join);
+    float2 *stat = reinterpret_cast<float2*>(smem + SM::stat), *sums = reinterpret_cast<float2*>(smem + SM::sums);
     if (__syncthreads_or(spoilt ? 1 : 0)) {
       // values that are no numbers where some row does not see them: straight from the definition
       for (int r = warp; r < rows; r += 4)
-        dense_row_to<T, D, true>(a, b, s.t0 + (row0 + r) / a.G, kvh * a.G + (row0 + r) % a.G, s, k0, k1, whole, a.few_o + static_cast<int64_t>(place + r) * D, a.few_ml + place + r);
+        dense_row_to<T, D, true>(a, b, s.t0 + (row0 + r) / a.G, kvh * a.G + (row0 + r) % a.G, s, k0, k1, whole,
+                                 SMALL ? join + r * SM::pitch : a.few_o + static_cast<int64_t>(place + r) * D, SMALL ? sums + r : a.few_ml + place + r);
+      if (SMALL && !whole) break;
       continue;
     }
     // the warps' rows, with their units
-    float* join = reinterpret_cast<float*>(smem + SM::join);
-    float2* stat = reinterpret_cast<float2*>(smem + SM::stat);
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
@@ -477,10 +518,45 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
           v.w = fmaf(x4.w, f[w], v.w);
         }
         if (whole) *reinterpret_cast<uint2*>(out + col) = make_uint2(narrow2<T>(v.x * inv, v.y * inv), narrow2<T>(v.z * inv, v.w * inv));
+        else if (SMALL) *reinterpret_cast<float4*>(join + r * SM::pitch + col) = v;        // (this thread has read what was there)
         else *reinterpret_cast<float4*>(a.few_o + static_cast<int64_t>(place + r) * D + col) = v;
       }
-      if (!whole && threadIdx.x % TPW == 0) a.few_ml[place + r] = make_float2(top, sum);
+      if (!whole && threadIdx.x % TPW == 0) (SMALL ? sums[r] : a.few_ml[place + r]) = make_float2(top, sum);
     }
+    if (SMALL) break;
+  }
+  if constexpr (SMALL) {
+    if (a.cta_share == 1) return;
+    // every CTA has a share of the columns of all rows: the parts' sums over the cluster, in the order of the keys
+    cluster_sync();
+    const DenseSeq s = walk.f.s;
+    const int row0 = walk.rt * R, rows = min(s.n * a.G - row0, R), share = a.cta_share, cols = D / share, rank = blockIdx.x % share;
+    for (int i = threadIdx.x; i < rows * (cols / 4); i += kFewThreads) {
+      const int r = i / (cols / 4), col = rank * cols + i % (cols / 4) * 4;
+      float top = -INFINITY, sum = 0.f;
+      float2 ml[8];
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        ml[p] = p < share ? ld_rank2(at_rank(sbase + SM::sums + r * 8, p)) : make_float2(-INFINITY, 0.f);
+        top = fmaxf(top, ml[p].x);
+      }
+      float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        if (ml[p].x == -INFINITY && ml[p].y == 0.f) continue;      // nothing of it is seen, or there is none
+        const float f = fast_exp2(ml[p].x - top);
+        const float4 v = ld_rank4(at_rank(sbase + SM::join + (r * SM::pitch + col) * 4, p));
+        sum = fmaf(ml[p].y, f, sum);
+        o4.x = fmaf(v.x, f, o4.x);
+        o4.y = fmaf(v.y, f, o4.y);
+        o4.z = fmaf(v.z, f, o4.z);
+        o4.w = fmaf(v.w, f, o4.w);
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const int t = s.t0 + (row0 + r) / a.G, head = walk.kvh * a.G + (row0 + r) % a.G;
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + head * a.q_hs + t * a.q_ts + col) = make_uint2(narrow2<T>(o4.x * inv, o4.y * inv), narrow2<T>(o4.z * inv, o4.w * inv));
+    }
+    cluster_sync();                                                // nobody leaves while its shared memory is read
   }
 }
 
@@ -518,6 +594,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
   const bool few = s.n * a.G <= a.few_rows;
   int parts, first = 0, row_of_few = 0;
   if (few) {
+    if (a.cta_share > 0) return;                                   // clusters leave nothing to join
     const int2 p = __ldcg(a.few_pieces + row);
     if (p.y < 0) return;
     first = p.x;
@@ -600,9 +677,23 @@ template <class T, int D>
 static int launch_few_t(const DenseArgs& a, cudaStream_t st) {
   auto go = [&](auto rows) {
     constexpr int NR = decltype(rows)::value;
-    const int r = ensure_dynamic_smem(reinterpret_cast<const void*>(&few_kernel<T, D, NR>), FewConf<D, NR>::total);
+    void (*kern)(DenseArgs) = a.cta_share > 0 ? few_kernel<T, D, NR, true> : few_kernel<T, D, NR, false>;
+    const int r = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), FewConf<D, NR>::total);
     if (r != FASTAR_OK) return r;
-    return launch_chained(few_kernel<T, D, NR>, a.few_ctas, kFewThreads, FewConf<D, NR>::total, st, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = a.cta_share;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = a.few_ctas;
+    cfg.blockDim = kFewThreads;
+    cfg.dynamicSmemBytes = FewConf<D, NR>::total;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = a.cta_share > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, a) == cudaSuccess ? FASTAR_OK : FASTAR_ERR_CUDA;
   };
   if constexpr (D == 64) {
     if (a.few_tile == 32) return go(std::integral_constant<int, 4>{});

@@ -529,10 +529,10 @@ def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_ne
             return kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new, max_len, frame_len, out)
     out = _out_like(torch, q, strides, out, where)
     nbytes = _workspace_bytes(B, T, max_new, max_len, H, KV, D)
-    work = torch.empty(nbytes, dtype=u8, device=q.device)
+    work = torch.empty(nbytes, dtype=u8, device=q.device) if nbytes > 16 else None           # (16: none is used)
     _check(lib.fastar_kv8_attention(q.data_ptr(), out.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
                                     table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
-                                    work.data_ptr(), nbytes, _raw_stream(dev)), "fastar_kv8_attention")
+                                    _ptr(work), nbytes, _raw_stream(dev)), "fastar_kv8_attention")
     return out
 
 

@@ -31,7 +31,7 @@ def packed_args(p, **kw):
 
 
 def attend_args(p, **kw):
-    a = dict(q=p, out=p + 2048, hs=BIG, ts=128, kc=p, vc=p, ks=p, vs=p, pages=4, PT=64, table=p, W=4, lens=p, cu=p, seqs=2, total=10, max_new=5, max_len=256, H=4, KV=2, D=128,
+    a = dict(q=p, out=p + 2048, hs=BIG, ts=128, kc=p, vc=p, ks=p, vs=p, pages=4, PT=64, table=p, W=400, lens=p, cu=p, seqs=2, total=10, max_new=5, max_len=25600, H=4, KV=2, D=128,
              dtype=0, frame=1, work=p, bytes=1 << 40, stream=None)
     a.update(kw)
     return list(a.values())
@@ -64,7 +64,7 @@ def test_packed_refusals(lib, mem, bad, status):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(q=None), -1), (dict(out=None), -1), (dict(kc=None), -1), (dict(vs=None), -1), (dict(table=None), -1), (dict(lens=None), -1), (dict(cu=None), -1), (dict(seqs=0), -1),
-    (dict(total=-1), -1), (dict(max_new=0), -1), (dict(max_len=4), -1), (dict(max_len=257), -1), (dict(pages=0), -1), (dict(W=0), -1), (dict(PT=32), -2), (dict(D=32), -2),
+    (dict(total=-1), -1), (dict(max_new=0), -1), (dict(max_len=4), -1), (dict(max_len=25601), -1), (dict(pages=0), -1), (dict(W=0), -1), (dict(PT=32), -2), (dict(D=32), -2),
     (dict(dtype=1), -1), (dict(frame=-2), -1), (dict(H=5), -1), (dict(work=None), -7), (dict(bytes=0), -7), (dict(ts=64), -1), (dict(hs=9), -1)])
 def test_paged_refusals(lib, mem, bad, status):
     assert lib.fastar_kv8_attention(*attend_args(mem[0], **bad)) == status
