@@ -46,8 +46,7 @@ struct ManySmem {
   static constexpr int k_off = 2 * q_tile, v_off = k_off + SK * q_tile, bar_off = v_off + SV * q_tile;
   static constexpr int scale_off = bar_off + 512;                  // [8][2] key scales of a tile's two halves
   static constexpr int misc_off = scale_off + 64;
-  static constexpr int factor_off = misc_off + 64;                 // [256]
-  static constexpr int total = factor_off + 1024;
+  static constexpr int total = misc_off + 64;
   static_assert(total <= 227 * 1024, "shared memory");
 };
 
@@ -94,8 +93,29 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   volatile int* done_flag = abort_flag + 2;                        // stays 0
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + SM::misc_off + 12);
   volatile float* unit_s = reinterpret_cast<volatile float*>(smem + SM::misc_off + 16);        // [4] by mover warp
-  volatile int* item_s = reinterpret_cast<volatile int*>(smem + SM::misc_off + 32);           // sequence, tile of it
+  volatile int* item_s = reinterpret_cast<volatile int*>(smem + SM::misc_off + 32);           // sequence, tile of it, and its DenseSeq
   const int warp = warp_index(), lane = threadIdx.x & 31;
+  if (threadIdx.x < kNumBars) {
+    const int i = threadIdx.x, role = i - kRoleBars;
+    // q; k_full, k_empty; v_full, v_empty, v_clean, v_asked; s, ld, p, pv, drain
+    const int count = i == 0 ? kMoveWarp : i < 1 + SK ? (PAGED ? 4 : 1) : i < 1 + 2 * SK ? 2 : i < 1 + 2 * SK + SV ? (PAGED ? 4 : 1) : i < 1 + 2 * SK + 2 * SV ? 2
+                      : i < 1 + 2 * SK + 3 * SV ? 4 : role < 0 ? 1 : role < 4 ? 2 : role < 12 ? 4 : 1;
+    mbar_init(bar + 8 * i, count);
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  if (!PAGED && warp == kKWarp && lane == 0) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  if (threadIdx.x == 0) {
+    item_s[0] = -1;
+    *abort_flag = *spoilt_s = *done_flag = 0;
+  }
+  tc_fence_before();
   chain_wait();
 
   // ---- the item: tiles of the sequences in order, a sequence's last (longest) first
@@ -103,15 +123,11 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
     int* red = reinterpret_cast<int*>(smem);                       // 17 words
     const int tile = blockIdx.x / a.KV;
     int64_t before = 0;
-    if (threadIdx.x == 0) {
-      item_s[0] = -1;
-      *abort_flag = *spoilt_s = *done_flag = 0;
-    }
     for (int b0 = 0; b0 < a.B && before <= tile; b0 += kManyThreads) {
       const int b = b0 + threadIdx.x;
       int mine = 0;
+      DenseSeq s;
       if (b < a.B) {
-        DenseSeq s;
         const int r = seq_of(a, b, s);
         if (r < 0 && a.status) record_status(a.status, kErrBounds);
         const int rows = s.n * a.G;
@@ -135,20 +151,27 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       if (mine > 0 && tile >= first && tile < first + mine) {
         item_s[0] = b;
         item_s[1] = mine - 1 - static_cast<int>(tile - first);
+        item_s[2] = s.t0;
+        item_s[3] = s.n;
+        item_s[4] = s.len;
       }
       before += all;
       __syncthreads();
     }
   }
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  chain_next();
   ManyItem it;
   it.b = item_s[0];
-  if (it.b < 0) return;
-  DenseSeq s;
-  seq_of(a, it.b, s);
+  const DenseSeq s{item_s[2], item_s[3], item_s[4]};
   it.kvh = blockIdx.x % a.KV;
   it.part = blockIdx.y;
   const bool whole = a.parts == 1 || s.len <= a.chunk;
-  if (whole ? it.part > 0 : static_cast<int64_t>(it.part) * a.chunk >= s.len) return;
+  if (it.b < 0 || (whole ? it.part > 0 : static_cast<int64_t>(it.part) * a.chunk >= s.len)) {        // nothing to do
+    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+    return;
+  }
   it.rows = s.n * a.G;
   it.row0 = item_s[1] * kRowsCta;
   it.past = s.len - s.n;
@@ -167,27 +190,6 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   const int nt = max(it.nt[0], it.nt[1]);
   const int clean_from = it.nt[1] > 0 ? (it.nt[0] > 0 ? min(it.whole_from[0], it.whole_from[1]) : it.whole_from[1]) : it.whole_from[0];
 
-  if (threadIdx.x < kNumBars) {
-    const int i = threadIdx.x, role = i - kRoleBars;
-    // q; k_full, k_empty; v_full, v_empty, v_clean, v_asked; s, ld, p, pv, drain
-    const int count = i == 0 ? 4 : i < 1 + SK ? (PAGED ? 4 : 1) : i < 1 + 2 * SK ? 2 : i < 1 + 2 * SK + SV ? (PAGED ? 4 : 1) : i < 1 + 2 * SK + 2 * SV ? 2
-                      : i < 1 + 2 * SK + 3 * SV ? 4 : role < 0 ? 1 : role < 4 ? 2 : role < 12 ? 4 : 1;
-    mbar_init(bar + 8 * i, count);
-    fence_mbar_init();
-  }
-  if (warp == kMmaWarp) {
-    tmem_alloc(smem_u32(tmem_slot), 512);
-    tmem_relinquish();
-  }
-  if (!PAGED && warp == kKWarp && lane == 0) {
-    tma_prefetch_desc(&tm_k);
-    tma_prefetch_desc(&tm_v);
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  chain_next();
 
   if (warp >= kMmaWarp) {
     set_regs<ManyRoles<D>::kRest>();
@@ -283,55 +285,6 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   } else if (warp >= kMoveWarp) {
     set_regs<ManyRoles<D>::kMove>();
     const int tid = threadIdx.x - kMoveWarp * 32;
-    // ================================================================ queries
-    const T* q = static_cast<const T*>(a.q);
-    if constexpr (!PAGED) {
-      constexpr int PPR = D / 8, RPP = 128 / PPR;                  // 16-byte pieces a row, rows a pass
-      const int piece = tid % PPR;
-#pragma unroll 4
-      for (int row = tid / PPR; row < kRowsCta; row += RPP) {
-        const int r = it.row0 + row;
-        const bool live = r < it.rows;
-        const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
-        cp_async16(sbase + (row >> 7) * SM::q_tile + tile_at16(row & 127, piece), q + head * a.q_hs + (s.t0 + i) * a.q_ts + piece * 8, live);
-      }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-    } else {
-      float* factor = reinterpret_cast<float*>(smem + SM::factor_off);
-#pragma unroll 1
-      for (int row = tid; row < kRowsCta; row += 128) {            // a thread a row: its largest, then fp16
-        const int r = it.row0 + row;
-        const bool live = r < it.rows;
-        const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
-        const uint4* src = reinterpret_cast<const uint4*>(q + head * a.q_hs + (s.t0 + i) * a.q_ts);
-        uint32_t most = 0;
-#pragma unroll 4
-        for (int p = 0; p < D / 8; ++p) {
-          const uint4 v = live ? __ldcg(src + p) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 f = widen2<T>((&v.x)[e]);
-            most = max(most, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
-          }
-        }
-        int e = static_cast<int>(most >> 23) - 127;
-        e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        factor[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (rsqrtf(static_cast<float>(D)) * 1.4426950408889634f);
-#pragma unroll 4
-        for (int p = 0; p < D / 8; ++p) {
-          uint4 v = live ? __ldcg(src + p) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float2 f = widen2<T>((&v.x)[w]);
-            (&v.x)[w] = narrow2<__half>(f.x * down, f.y * down);
-          }
-          sts128(sbase + (row >> 7) * SM::q_tile + tile_at16(row & 127, p), v);
-        }
-      }
-    }
-    fence_proxy_async_smem();
-    mbar_arrive_warp(bar_q);
     bool spoilt = false;
     if constexpr (!PAGED) {
       // ================================================================ V of tiles that some row does not see as a whole
@@ -489,9 +442,59 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
     const uint32_t lane_t = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_t = lane_t + t * 128, o_t = lane_t + 256 + t * D;
     float factor = rsqrtf(static_cast<float>(D)) * 1.4426950408889634f;
-    if (PAGED && n > 0) {
-      mbar_wait_warp(bar_q, 0, abort_flag, a.status);
-      factor = reinterpret_cast<const float*>(smem + SM::factor_off)[row];
+    // ---- this warp's 32 queries, PPR lanes a row
+    constexpr int PPR = D / 8, RPI = 32 / PPR;                     // 16-byte pieces a row, rows at once
+    const int my_row = lane / PPR, piece = lane % PPR;
+    {
+      const T* mine = static_cast<const T*>(a.q) + head * a.q_hs + (s.t0 + i) * a.q_ts;
+      const uint32_t tile = sbase + t * SM::q_tile;
+      const unsigned lives = __ballot_sync(0xffffffffu, live);
+      auto from = [&](int r2) { return reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r2)) + piece * 8; };
+      if constexpr (!PAGED) {
+#pragma unroll 4
+        for (int p = 0; p < PPR; ++p) {
+          const int r2 = p * RPI + my_row;
+          cp_async16(tile + tile_at16((warp & 3) * 32 + r2, piece), from(r2), (lives >> r2) & 1);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+      } else {
+        const float scale = factor;
+#pragma unroll 1
+        for (int p0 = 0; p0 < PPR; p0 += 4) {
+          uint4 v[4];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const int r2 = (p0 + p) * RPI + my_row;
+            const T* src = from(r2);
+            v[p] = (lives >> r2) & 1 ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = widen2<T>((&v[p].x)[e]);
+              most = max(most, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+            }
+#pragma unroll
+            for (int w = 1; w < PPR; w <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, w));
+            int e = static_cast<int>(most >> 23) - 127;
+            e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));            // (a row that is not finite stays as it is)
+            const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * scale;
+            // what the row was divided by goes to the thread that has it
+            const float theirs = __shfl_sync(0xffffffffu, up, lane % RPI * PPR);
+            if (lane / RPI == p0 + p) factor = theirs;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const float2 f = widen2<T>((&v[p].x)[w]);
+              (&v[p].x)[w] = narrow2<__half>(f.x * down, f.y * down);
+            }
+            sts128(tile + tile_at16((warp & 3) * 32 + (p0 + p) * RPI + my_row, piece), v[p]);
+          }
+        }
+      }
+      fence_proxy_async_smem();
+      mbar_arrive_warp(bar_q);
     }
     float m = -INFINITY;
     float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -602,30 +605,46 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
     const int64_t part_row = (static_cast<int64_t>(it.part) * a.T + tok) * a.H + head;
     const float inv = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
     T* out = static_cast<T*>(a.out) + head * a.q_hs + tok * a.q_ts;
-    if (ok) {
+    // Rows go through the place of the warp's queries, D 16-bit columns (half as many 32-bit ones) at a time, so that a store writes whole rows
+    if (ok && n > 0) {
+      const uint32_t tile = sbase + t * SM::q_tile;
+      const unsigned lives = __ballot_sync(0xffffffffu, live);
+      uint8_t* mine = whole ? reinterpret_cast<uint8_t*>(out) : reinterpret_cast<uint8_t*>(a.part_o + part_row * D);
 #pragma unroll 1
-      for (int q4 = 0; q4 < D / 32 && n > 0; ++q4) {
-        uint32_t v[32];
-        tmem_ld32(o_t + q4 * 32, v);
-        tmem_wait_ld();
-        if (!live) continue;
+      for (int half = 0; half < (whole ? 1 : 2); ++half) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < (whole ? D : D / 2); c0 += 32) {
+          uint32_t v[32];
+          tmem_ld32(o_t + half * (D / 2) + c0, v);
+          tmem_wait_ld();
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = sum == 0.f ? 0u : __float_as_uint(__uint_as_float(v[e]) * inv);
-        if (whole) {
+          for (int e = 0; e < 32; ++e) v[e] = sum == 0.f ? 0u : __float_as_uint(__uint_as_float(v[e]) * inv);
+          if (whole) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint4 o;
+            for (int e = 0; e < 4; ++e) {
+              uint4 o;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) (&o.x)[w] = narrow2<T>(__uint_as_float(v[8 * e + 2 * w]), __uint_as_float(v[8 * e + 2 * w + 1]));
-            *reinterpret_cast<uint4*>(out + q4 * 32 + 8 * e) = o;
+              for (int w = 0; w < 4; ++w) (&o.x)[w] = narrow2<T>(__uint_as_float(v[8 * e + 2 * w]), __uint_as_float(v[8 * e + 2 * w + 1]));
+              sts128(tile + tile_at16(row & 127, c0 / 8 + e), o);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sts128(tile + tile_at16(row & 127, c0 / 4 + e), make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]));
           }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(a.part_o + part_row * D + q4 * 32 + 4 * e) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
         }
+        __syncwarp();
+#pragma unroll 4
+        for (int p = 0; p < PPR; ++p) {
+          const int r2 = p * RPI + my_row;
+          uint8_t* to = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r2)) + half * (D * 2) + piece * 16;
+          uint4 o;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w) : "r"(tile + tile_at16((warp & 3) * 32 + r2, piece)));
+          if ((lives >> r2) & 1) *reinterpret_cast<uint4*>(to) = o;
+        }
+        __syncwarp();
       }
-      if (!whole && live) a.part_ml[part_row] = make_float2(m, sum);
     }
+    if (ok && !whole && live) a.part_ml[part_row] = make_float2(m, sum);
   }
   tc_fence_before();
   __syncthreads();
