@@ -167,7 +167,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   const DenseSeq s{item_s[2], item_s[3], item_s[4]};
   it.kvh = blockIdx.x % a.KV;
   it.part = blockIdx.y;
-  const bool whole = a.parts == 1 || s.len <= a.chunk;
+  const bool whole = !PAGED || a.parts == 1 || s.len <= a.chunk;     // (packed: the keys are never cut)
   if (it.b < 0 || (whole ? it.part > 0 : static_cast<int64_t>(it.part) * a.chunk >= s.len)) {        // nothing to do
     if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
     return;
@@ -435,18 +435,33 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   } else {
     // ================================================================== soft-max of query tile t, a thread a row
     set_regs<ManyRoles<D>::kSoftmax>();
-    const int t = warp >> 2, row = t * 128 + (threadIdx.x & 127), r = it.row0 + row, n = it.nt[t];
-    const bool live = r < it.rows;
-    const int i = live ? r / a.G : 0, head = it.kvh * a.G + (live ? r - i * a.G : 0);
-    const int end = live ? visible_end(it.past + i, s.len, a.frame) - it.k0 : 0;       // in the keys of the part
+    const int t = warp >> 2, n = it.nt[t];
+    constexpr int PPR = D / 8, RPI = 32 / PPR;                     // 16-byte pieces a row, rows that a warp reads or writes at once
+    struct Row {
+      int r, i, head;                                              // row of the sequence, its token and query head
+      bool live;
+    };
+    // (asked for before and after the loop, so that it does not live through it)
+    auto row_of = [&](int at) {
+      asm volatile("" : "+r"(at));
+      Row w;
+      w.r = it.row0 + at;
+      w.live = w.r < it.rows;
+      w.i = w.live ? w.r / a.G : 0;
+      w.head = it.kvh * a.G + (w.live ? w.r - w.i * a.G : 0);
+      return w;
+    };
     const uint32_t lane_t = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_t = lane_t + t * 128, o_t = lane_t + 256 + t * D;
     float factor = rsqrtf(static_cast<float>(D)) * 1.4426950408889634f;
+    int end;                                                       // of the keys that this thread's row sees, from the part's first on
     // ---- this warp's 32 queries, PPR lanes a row
-    constexpr int PPR = D / 8, RPI = 32 / PPR;                     // 16-byte pieces a row, rows at once
-    const int my_row = lane / PPR, piece = lane % PPR;
     {
-      const T* mine = static_cast<const T*>(a.q) + head * a.q_hs + (s.t0 + i) * a.q_ts;
+      const Row w = row_of(threadIdx.x);
+      const bool live = w.live;
+      end = live ? visible_end(it.past + w.i, s.len, a.frame) - it.k0 : 0;
+      const int my_row = lane / PPR, piece = lane % PPR;
+      const T* mine = static_cast<const T*>(a.q) + w.head * a.q_hs + (s.t0 + w.i) * a.q_ts;
       const uint32_t tile = sbase + t * SM::q_tile;
       const unsigned lives = __ballot_sync(0xffffffffu, live);
       auto from = [&](int r2) { return reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r2)) + piece * 8; };
@@ -601,13 +616,16 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
     const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y);
     float unit = 1.f;
     if (PAGED && n > 0) unit = fmaxf(fmaxf(unit_s[0], unit_s[1]), fmaxf(unit_s[2], unit_s[3]));
-    const int tok = s.t0 + i;
-    const int64_t part_row = (static_cast<int64_t>(it.part) * a.T + tok) * a.H + head;
+    const Row w = row_of(threadIdx.x);
+    const bool live = w.live;
+    const int tok = s.t0 + w.i, row = threadIdx.x;
+    const int64_t part_row = (static_cast<int64_t>(it.part) * a.T + tok) * a.H + w.head;
     const float inv = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
-    T* out = static_cast<T*>(a.out) + head * a.q_hs + tok * a.q_ts;
+    T* out = static_cast<T*>(a.out) + w.head * a.q_hs + tok * a.q_ts;
     // Rows go through the place of the warp's queries, D 16-bit columns (half as many 32-bit ones) at a time, so that a store writes whole rows
     if (ok && n > 0) {
       const uint32_t tile = sbase + t * SM::q_tile;
+      const int my_row = lane / PPR, piece = lane % PPR;
       const unsigned lives = __ballot_sync(0xffffffffu, live);
       uint8_t* mine = whole ? reinterpret_cast<uint8_t*>(out) : reinterpret_cast<uint8_t*>(a.part_o + part_row * D);
 #pragma unroll 1
