@@ -438,6 +438,15 @@ int fastar_packed_attention(const void* q, const void* k, const void* v, void* o
                             int32_t max_tokens, int32_t num_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype, int32_t frame_len,
                             void* stream);
 
+/* The four calls above with their arguments, in the same order, as `count` 64-bit numbers (pointers and sizes by value), for bindings in which
+ * every argument costs: Python's ctypes takes 2.3 us to convert the 26 of fastar_kv8_attention one by one, 0.6 in this form, and the call's kernel is
+ * launched in as much.  FASTAR_ERR_INVALID_ARG if `count` is not the call's or a 32-bit argument is out of range. */
+#define FASTAR_DENSE_TABLES    0
+#define FASTAR_DENSE_APPEND    1
+#define FASTAR_DENSE_ATTENTION 2
+#define FASTAR_DENSE_PACKED    3
+int fastar_dense_call(int32_t call, const void* args, int32_t count);
+
 /* Synchronises `stream`, returns FASTAR_OK or the first error a kernel of the dense path recorded on the current device since the last read,
  * and clears it.  Not for use during stream capture. */
 int fastar_dense_last_status(void* stream);

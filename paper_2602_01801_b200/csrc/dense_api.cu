@@ -1,7 +1,11 @@
 // C entries of the dense path (include/fastar.h): argument checks and the choice of kernels.  No device memory is allocated here.
 #include <cudaTypedefs.h>
 
+#include <cstring>
 #include <mutex>
+#include <tuple>
+#include <type_traits>
+#include <utility>
 
 #include "common.h"
 #include "dense.h"
@@ -252,6 +256,42 @@ extern "C" int fastar_packed_attention(const void* q, const void* k, const void*
   if (r == FASTAR_OK) r = encode_packed(&tm_v, v, head_dim, total_tokens, num_kv_heads, kv_token_stride, kv_head_stride, fp16);
   if (r != FASTAR_OK) return r;
   return launch_dense_many(a, tm_k, tm_v, head_dim, fp16, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+template <class A>
+A from_word(int64_t w, bool& ok) {
+  if constexpr (std::is_pointer<A>::value) {
+    return reinterpret_cast<A>(static_cast<uintptr_t>(w));
+  } else {
+    const A a = static_cast<A>(w);
+    if (static_cast<int64_t>(a) != w) ok = false;
+    return a;
+  }
+}
+template <class... A, size_t... I>
+int call_with(int (*f)(A...), const int64_t* w, std::index_sequence<I...>) {
+  bool ok = true;
+  const std::tuple<A...> args{from_word<A>(w[I], ok)...};
+  return ok ? f(std::get<I>(args)...) : FASTAR_ERR_INVALID_ARG;
+}
+template <class... A>
+int call_with(int (*f)(A...), const void* args, int32_t count) {
+  if (!args || count != static_cast<int32_t>(sizeof...(A))) return FASTAR_ERR_INVALID_ARG;
+  int64_t w[sizeof...(A)];
+  std::memcpy(w, args, sizeof(w));
+  return call_with(f, w, std::make_index_sequence<sizeof...(A)>());
+}
+}  // namespace
+
+extern "C" int fastar_dense_call(int32_t call, const void* args, int32_t count) {
+  switch (call) {
+    case FASTAR_DENSE_TABLES: return call_with(fastar_block_tables, args, count);
+    case FASTAR_DENSE_APPEND: return call_with(fastar_kv8_append, args, count);
+    case FASTAR_DENSE_ATTENTION: return call_with(fastar_kv8_attention, args, count);
+    case FASTAR_DENSE_PACKED: return call_with(fastar_packed_attention, args, count);
+    default: return FASTAR_ERR_INVALID_ARG;
+  }
 }
 
 extern "C" int fastar_dense_last_status(void* stream) {

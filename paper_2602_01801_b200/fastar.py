@@ -6,6 +6,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -71,6 +72,7 @@ SIGNATURES = {
     "fastar_kv8_attention_workspace_bytes": (C.c_size_t, [_i32] * 7),
     "fastar_kv8_attention": (C.c_int, [_vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 9 + [_vp, C.c_size_t, _vp]),
     "fastar_packed_attention": (C.c_int, [_vp] * 4 + [_i64] * 4 + [_vp] + [_i32] * 8 + [_vp]),
+    "fastar_dense_call": (C.c_int, [_i32, C.c_char_p, _i32]),
     "fastar_dense_last_status": (C.c_int, [_vp]),
     "fastar_profile_enable": (C.c_int, [_vp, _i32]),
     "fastar_profile_read": (C.c_int, [_vp, _vp, _vp, _vp]),
@@ -430,7 +432,8 @@ def noalloc_last_status() -> int:
 # fp8 e4m3 codes) with scales [pages][kv heads] (fp32), and a table [sequences][width] of pages.  Full rules: include/fastar.h.
 # A call of these takes the GPU a few microseconds at the smallest, so what the host does for one counts: tensors are looked at once each, by the
 # cheapest of their attributes.
-_dense = None                # (library, torch, dtype codes, int32, uint8, float32, current device), once it is loaded
+_TABLES, _APPEND, _ATTENTION, _PACKED = ((i, struct.Struct(f"{n}q").pack, n) for i, n in enumerate((15, 20, 26, 18)))      # fastar_dense_call's
+_dense = None                # (its function, torch, dtype codes, int32, uint8, float32, current device), once it is loaded
 
 
 def _dense_init():
@@ -438,7 +441,7 @@ def _dense_init():
     import torch
     if _raw_stream is None:
         _find_raw_stream(torch)
-    _dense = (load_library(), torch, {torch.bfloat16: BF16, torch.float16: FP16}, torch.int32, torch.uint8, torch.float32, torch.cuda.current_device)
+    _dense = (load_library().fastar_dense_call, torch, {torch.bfloat16: BF16, torch.float16: FP16}, torch.int32, torch.uint8, torch.float32, torch.cuda.current_device)
     return _dense
 
 
@@ -490,8 +493,9 @@ def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add:
     B = held.shape[0]
     cu, lens, first_out = torch.split_with_sizes(torch.empty(2 * B + 2, dtype=i32, device=held.device), (B + 1, B, 1))
     slots = torch.empty(max_add, dtype=torch.int64, device=held.device)
-    _check(lib.fastar_block_tables(held.data_ptr(), add.data_ptr(), B, page_tokens, free_pages.data_ptr(), free_pages.shape[0], first.data_ptr(), table.data_ptr(),
-                                   table.shape[1], cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), max_add, first_out.data_ptr(), _raw_stream(dev)), "fastar_block_tables")
+    call, pack, count = _TABLES
+    _check(lib(call, pack(held.data_ptr(), add.data_ptr(), B, page_tokens, free_pages.data_ptr(), free_pages.shape[0], first.data_ptr(), table.data_ptr(),
+                table.shape[1], cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), max_add, first_out.data_ptr(), _raw_stream(dev)), count), "fastar_block_tables")
     return dict(cu=cu, lens=lens, slots=slots, first=first_out)
 
 
@@ -509,8 +513,9 @@ def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu
     if dev != current():
         with torch.cuda.device(dev):
             return kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu)
-    _check(lib.fastar_kv8_append(k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
-                                 P, PT, table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, shape[1], KV, D, dtype, _raw_stream(dev)), "fastar_kv8_append")
+    call, pack, count = _APPEND
+    _check(lib(call, pack(k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                P, PT, table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, shape[1], KV, D, dtype, _raw_stream(dev)), count), "fastar_kv8_append")
 
 
 def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new: int, max_len: int, frame_len: int = 1, out=None):
@@ -530,9 +535,10 @@ def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_ne
     out = _out_like(torch, q, strides, out, where)
     nbytes = _workspace_bytes(B, T, max_new, max_len, H, KV, D)
     work = torch.empty(nbytes, dtype=u8, device=q.device) if nbytes > 16 else None           # (16: none is used)
-    _check(lib.fastar_kv8_attention(q.data_ptr(), out.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
-                                    table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
-                                    _ptr(work), nbytes, _raw_stream(dev)), "fastar_kv8_attention")
+    call, pack, count = _ATTENTION
+    _check(lib(call, pack(q.data_ptr(), out.data_ptr(), strides[0], strides[1], k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, PT,
+                table.data_ptr(), table.shape[1], lens.data_ptr(), cu.data_ptr(), B, T, max_new, max_len, H, KV, D, dtype, frame_len,
+                0 if work is None else work.data_ptr(), nbytes, _raw_stream(dev)), count), "fastar_kv8_attention")
     return out
 
 
@@ -550,8 +556,9 @@ def packed_attention(q, k, v, cu, max_tokens: int, frame_len: int = 1, out=None)
         with torch.cuda.device(dev):
             return packed_attention(q, k, v, cu, max_tokens, frame_len, out)
     out = _out_like(torch, q, strides, out, where)
-    _check(lib.fastar_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), strides[0], strides[1], kv_strides[0], kv_strides[1], cu.data_ptr(),
-                                       cu.shape[0] - 1, shape[1], max_tokens, shape[0], kv_shape[0], shape[2], dtype, frame_len, _raw_stream(dev)), "fastar_packed_attention")
+    call, pack, count = _PACKED
+    _check(lib(call, pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), strides[0], strides[1], kv_strides[0], kv_strides[1], cu.data_ptr(),
+                cu.shape[0] - 1, shape[1], max_tokens, shape[0], kv_shape[0], shape[2], dtype, frame_len, _raw_stream(dev)), count), "fastar_packed_attention")
     return out
 
 

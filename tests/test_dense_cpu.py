@@ -92,6 +92,27 @@ def test_table_refusals(lib, mem, bad, status):
     assert lib.fastar_block_tables(*table_args(p, slots=p + 4)) == -1
 
 
+def test_arguments_as_words(lib, mem):
+    """fastar_dense_call takes the calls' arguments as 64-bit words and answers as they do; a count or a 32-bit argument that is not theirs is refused."""
+    from paper_2602_01801_b200 import fastar
+    p = mem[0]
+    for (call, pack, n), args, bad in ((fastar._TABLES, table_args, dict(PT=100)), (fastar._APPEND, append_args, dict(D=80)), (fastar._ATTENTION, attend_args, dict(PT=32)),
+                                       (fastar._PACKED, packed_args, dict(D=96))):
+        words = [0 if a is None else a for a in args(p, **bad)]
+        assert len(words) == n
+        assert lib.fastar_dense_call(call, pack(*words), n) == -2
+        assert lib.fastar_dense_call(call, pack(*words), n - 1) == -1
+        assert lib.fastar_dense_call(call, None, n) == -1
+        for i in (i for i, v in enumerate(words) if 0 < v < 1000):
+            wide = list(words)
+            wide[i] += 1 << 32
+            assert lib.fastar_dense_call(call, pack(*wide), n) in (-1, -2)
+    assert lib.fastar_dense_call(4, b"", 0) == -1 and lib.fastar_dense_call(-1, b"", 0) == -1
+    words = packed_args(p, seqs=2 + (1 << 32))
+    words[-1] = 0
+    assert lib.fastar_dense_call(3, fastar._PACKED[1](*words), 18) == -1
+
+
 def test_workspace_sizes(lib):
     size = lib.fastar_kv8_attention_workspace_bytes
     assert size(1, 0, 1, 1, 1, 1, 64) >= 16
