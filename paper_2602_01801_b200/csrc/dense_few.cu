@@ -13,6 +13,9 @@
 //   - A page's value scale is a unit of the accumulators: they are multiplied by a power of two where it changes from page to page, exactly.  The unit is kept
 //     within 2^60 of the largest seen, so that a page of zeros (scale 2^-126) does not take the sums out of range.
 //   - The row sums add up the probabilities as rounded.
+// Measured (B200, us): one token each of eight sequences of 65 536 keys, 40 query and 8 key heads 172 (6.2 TB/s of codes, 187 at the power limit), with rows as the products'
+// first operand, 16 of them, and a CTA for every 4 096 keys 282; of 32 sequences of 1 to 16 384 keys 65 (4.9 TB/s) after 134; of 512 sequences of up to 1 000 keys 89-102.
+// Two CTAs an SM with tiles of 32 keys: 67, 121 for the last two.
 #include "common.h"
 #include "dense.h"
 #include "dense_rows.cuh"

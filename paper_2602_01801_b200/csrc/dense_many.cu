@@ -1,19 +1,27 @@
 // Dense attention for sequences with many rows: packed prompts over their own keys (TMA), and chunks over the 8-bit cache (codes converted on the way).
 //
 // The rows of a key head are (token, query head) pairs, token-major, so that G query heads that share keys share their tiles, and a causal limit moves by one
-// every G rows.  A CTA takes 256 of them as two query tiles of 128 (TMEM lanes) and walks the key tiles of 128:
+// token every G rows.  A CTA takes 256 of them as two query tiles of 128 (TMEM lanes) and walks the key tiles of 128, in parts of kSub keys:
 //   S_t  = Q_t K_j^T              tcgen05.mma, shared memory x shared memory -> TMEM
-//   P_t  = exp2(S_t f - m)        a thread a row; P_t takes the place of S_t's first half in TMEM
+//   P_t  = exp2(S_t f - m)        a thread a row
 //   O_t += P_t V_j                tcgen05.mma, TMEM x shared memory
-// While one tile is in its exponentials the tensor core has the other's products: 2 x 1 060 cycles of MMAs against 2 x 1 024 of the special-function units per
-// key tile, so an eighth of the exponentials goes to the FMA units.  The running maximum is raised only when a logit exceeds it by 8 binary orders (O is
-// rescaled then, by the warps that own its rows); sums add up the probabilities as rounded.
-// 8-bit cache: four warps read codes, convert them to fp16 (exact) and put them where TMA would have put them.  Queries are fp16 too, their row divided by a
-// power of two; a page's key scale goes into the factor of the logits, value scales are taken relative to the largest of the CTA's keys (a power of two, so
-// nothing is rounded within 2^15 of it; beyond that, and where there are NaN codes, the rows are worked out from the definition).
+// TMEM holds two S of 128 columns and two O of d.  At d = 128 that is all of it: P takes the place of its S, and a tile goes in two halves of 64 keys, so that the
+// products of one half run while the other is in its exponentials.  At d = 64 P lies beside, and Q K^T of the next tile follows as soon as the logits are in registers.
+// The running maximum is raised only when a logit exceeds it by 8 binary orders (O is rescaled then, by the warps that own its rows); sums add up the
+// probabilities as rounded.  Three of sixteen pairs of exponentials go to the FMA units.
+// 8-bit cache: four warps read codes, two tiles ahead in registers, convert them to fp16 (exact) and put them where TMA would have put them.  Queries are fp16
+// too, their row divided by a power of two; a page's key scale goes into the factor of the logits, value scales are taken relative to the largest of the
+// CTA's keys (a power of two, so nothing is rounded within 2^15 of it; beyond that, and where there are NaN codes in a tile that some row does not see as a whole,
+// the rows are worked out from the definition).
 // What a row does not see must not reach it: V rows behind the last visible key are zeroed, and values that are not finite in a tile that some row does not see as
 // a whole are taken out, and all rows of the CTA are worked out from the definition afterwards (dense_rows.cuh).
-// Warp roles: 0-3 and 4-7 soft-max of the two tiles, 8-11 Q, and the codes' way in (or the look at V), 12 MMAs, 13 K, 14 V (TMA).
+// What bounds it: at d = 128 the card's power limit (990 W, 1.7 GHz of 1.965): tensor pipe 0.51 of the cycles packed, 0.40 with codes; exponentials 0.42 and 0.36.  At
+// d = 64 the soft-max warps' chain of load, maximum, exponentials, store.
+// Measured (B200, us): 16 384 tokens, 8 query and 2 key heads 515-530 (1.05 PFLOP/s); one warp issuing for both tiles, whole tiles of 128, 520-540; the same at d = 64
+// 396, whole tiles with P over S 445.  Three times 4 680 tokens, 12 heads, by frames 292-317.  1 560 queries over 29 640 8-bit keys, 12 heads 369-375: with the codes
+// one tile ahead and NaN and scale work in every tile 614, whole tiles 455, queries by one warpgroup row by row and outputs by thread 396.  What an item costs beside its
+// tiles: some 5 000 cycles, 14 500 with queries and outputs that way (25 000 over codes).
+// Warp roles: 0-3 and 4-7 soft-max of the two tiles (and their queries and outputs), 8-11 the codes' way in (or the look at V), 12 and 13 MMAs of the two tiles, 14 K, 15 V (TMA).
 #include <cudaTypedefs.h>
 
 #include "common.h"
