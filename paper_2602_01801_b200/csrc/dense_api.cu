@@ -58,6 +58,8 @@ int shape_ok(int H, int KV, int D, int dtype) {
 // Rows and positions are counted in 32 bits.
 constexpr int64_t kMostRows = int64_t{1} << 30;
 bool too_long(int total, int max_len, int H) { return static_cast<int64_t>(total) * H > kMostRows || max_len > kMostRows; }
+// ... and shares of all tiles in 64: sequences x key heads x tiles x CTAs
+bool too_many(int seqs, int max_len, int KV) { return seqs > (1 << 20) || static_cast<int64_t>(seqs) * KV * (max_len / kFewKeys + 1) > (int64_t{1} << 50); }
 // Tiles of 128 tokens x 64 columns of a packed tensor [heads][T][d].
 int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int heads, int64_t ts, int64_t hs, bool fp16) {
   if (tokens == 1) ts = d;                                         // (a stride over one token or one head is not used)
@@ -169,7 +171,7 @@ extern "C" int fastar_kv8_append(const void* k_new, const void* v_new, int64_t h
   if (total_tokens == 0) return FASTAR_OK;
   if (!rows_ok(k_new, head_stride, token_stride, num_kv_heads, total_tokens, head_dim) || !rows_ok(v_new, head_stride, token_stride, num_kv_heads, total_tokens, head_dim))
     return FASTAR_ERR_INVALID_ARG;
-  if (too_long(total_tokens, 1, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (too_long(total_tokens, 1, num_kv_heads) || too_many(num_seqs, 1, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   AppendArgs a{};
   a.k = k_new; a.v = v_new; a.hs = head_stride; a.ts = token_stride;
   a.T = total_tokens; a.B = num_seqs; a.KV = num_kv_heads; a.D = head_dim; a.PT = page_tokens; a.W = table_width; a.pages = num_pages;
@@ -183,7 +185,7 @@ extern "C" int fastar_kv8_append(const void* k_new, const void* v_new, int64_t h
 extern "C" size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
                                                        int32_t num_kv_heads, int32_t head_dim) {
   if (shape_ok(num_heads, num_kv_heads, head_dim, FASTAR_BF16) != FASTAR_OK || num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new ||
-      too_long(total_tokens, max_len, num_heads))
+      too_long(total_tokens, max_len, num_heads) || too_many(num_seqs, max_len, num_kv_heads))
     return 0;
   return attend_plan(num_seqs, total_tokens, max_new, max_len, num_heads, num_kv_heads, head_dim).bytes;
 }
@@ -198,7 +200,7 @@ extern "C" int fastar_kv8_attention(const void* q, void* out, int64_t head_strid
   if (num_seqs < 1 || total_tokens < 0 || max_new < 1 || max_len < max_new || frame_len < 0 || num_pages < 1 || table_width < 1) return FASTAR_ERR_INVALID_ARG;
   if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (max_len > static_cast<int64_t>(table_width) * page_tokens) return FASTAR_ERR_INVALID_ARG;
-  if (too_long(total_tokens, max_len, num_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (too_long(total_tokens, max_len, num_heads) || too_many(num_seqs, max_len, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (!table || !lens || !cu || !aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
   if (!k_codes || !v_codes || !k_scale || !v_scale || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
     return FASTAR_ERR_INVALID_ARG;
@@ -235,7 +237,7 @@ extern "C" int fastar_packed_attention(const void* q, const void* k, const void*
   int r = shape_ok(num_heads, num_kv_heads, head_dim, dtype);
   if (r != FASTAR_OK) return r;
   if (num_seqs < 1 || total_tokens < 0 || max_tokens < 1 || frame_len < 0 || !cu || !aligned(cu, 4)) return FASTAR_ERR_INVALID_ARG;
-  if (too_long(total_tokens, max_tokens, num_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if (too_long(total_tokens, max_tokens, num_heads) || too_many(num_seqs, 1, num_kv_heads)) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (total_tokens == 0) return FASTAR_OK;
   if (!rows_ok(q, head_stride, token_stride, num_heads, total_tokens, head_dim) || !rows_ok(out, head_stride, token_stride, num_heads, total_tokens, head_dim) || q == out)
     return FASTAR_ERR_INVALID_ARG;

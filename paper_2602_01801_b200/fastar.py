@@ -533,6 +533,7 @@ def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_ne
         with torch.cuda.device(dev):
             return kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new, max_len, frame_len, out)
     out = _out_like(torch, q, strides, out, where)
+    max_new, max_len = int(max_new), int(max_len)
     nbytes = _workspace_bytes(B, T, max_new, max_len, H, KV, D)
     work = torch.empty(nbytes, dtype=u8, device=q.device) if nbytes > 16 else None           # (16: none is used)
     call, pack, count = _ATTENTION

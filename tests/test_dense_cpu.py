@@ -52,7 +52,7 @@ def table_args(p, **kw):
 @pytest.mark.parametrize("bad,status", [
     (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(out=None), -1), (dict(cu=None), -1), (dict(seqs=0), -1), (dict(total=-1), -1), (dict(max=0), -1),
     (dict(H=3), -1), (dict(KV=0), -1), (dict(H=1), -1), (dict(D=96), -2), (dict(dtype=1), -1), (dict(dtype=3), -1), (dict(frame=-1), -1), (dict(ts=64), -1),
-    (dict(kts=120), -1), (dict(hs=100), -1), (dict(max=2 ** 30 + 1), -2), (dict(total=2 ** 29), -2), (dict(ts=132), -1), (dict(khs=0), -1), (dict(hs=-BIG), -1)])
+    (dict(kts=120), -1), (dict(hs=100), -1), (dict(max=2 ** 30 + 1), -2), (dict(seqs=2 ** 20 + 1), -2), (dict(total=2 ** 29), -2), (dict(ts=132), -1), (dict(khs=0), -1), (dict(hs=-BIG), -1)])
 def test_packed_refusals(lib, mem, bad, status):
     assert lib.fastar_packed_attention(*packed_args(mem[0], **bad)) == status
     if "q" in bad:
@@ -116,7 +116,7 @@ def test_arguments_as_words(lib, mem):
 def test_workspace_sizes(lib):
     size = lib.fastar_kv8_attention_workspace_bytes
     assert size(1, 0, 1, 1, 1, 1, 64) >= 16
-    for bad in ((0, 1, 1, 1, 1, 1, 64), (1, -1, 1, 1, 1, 1, 64), (1, 1, 0, 1, 1, 1, 64), (1, 1, 2, 1, 1, 1, 64), (1, 1, 1, 1, 3, 2, 64), (1, 1, 1, 1, 1, 1, 96), (1, 1, 1, 2 ** 30 + 1, 1, 1, 64), (1, 2 ** 29, 1, 1, 4, 1, 64)):
+    for bad in ((0, 1, 1, 1, 1, 1, 64), (1, -1, 1, 1, 1, 1, 64), (1, 1, 0, 1, 1, 1, 64), (1, 1, 2, 1, 1, 1, 64), (1, 1, 1, 1, 3, 2, 64), (1, 1, 1, 1, 1, 1, 96), (1, 1, 1, 2 ** 30 + 1, 1, 1, 64), (1, 2 ** 29, 1, 1, 4, 1, 64), (2 ** 20 + 1, 1, 1, 1, 1, 1, 64), (2 ** 20, 1, 1, 2 ** 30, 60000, 60000, 64)):
         assert size(*bad) == 0
     # never beyond one part for every 128 keys and row, and two pieces of 32 rows for each of 592 CTAs
     for args in ((1, 1, 1, 65536, 40, 8, 128), (64, 64, 1, 16384, 16, 4, 64), (3, 4680, 1560, 32768, 12, 12, 128), (1, 1, 1, 2 ** 30, 1, 1, 128)):

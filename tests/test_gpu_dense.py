@@ -258,22 +258,55 @@ def test_paged_flat_and_peaked_rows(fastar, std, n):
     paged(fastar, "fp16", 64, 4, 2, [n, n], [2500, 90], std=std)
 
 
+@pytest.mark.parametrize("D,H,KV", [(64, 2, 1), (128, 3, 3)])
+def test_paged_many_sequences(fastar, D, H, KV):
+    # more sequences than a CTA has threads; some without new tokens; of few rows, and with one of many among them
+    g = gen(21)
+    past = torch.randint(0, 700, (290,), generator=g, device=DEV).tolist()
+    past[17], past[200] = 5000, 9000
+    ns = [0 if b % 11 == 3 else 1 + (b % 5 == 2) for b in range(290)]
+    paged(fastar, "bf16", D, H, KV, ns, past)
+    ns[130] = 90
+    paged(fastar, "bf16", D, H, KV, ns, past)
+
+
+def test_packed_many_sequences(fastar):
+    packed(fastar, "bf16", 64, 2, 1, [(7 * b) % 6 for b in range(700)] + [300], 1)
+
+
+def test_nothing_to_do(fastar):
+    q = torch.zeros(4, 0, 64, dtype=torch.bfloat16, device=DEV)
+    pool = Pool(2, 2, 64, 64)
+    assert fastar.packed_attention(q, q[:2], q[:2], i32([0, 0]), 1).shape == (4, 0, 64)
+    fastar.kv8_append(q[:2], q[:2], *pool.args(), i32([[0]]), i32([5]), i32([0, 0]))
+    assert fastar.kv8_attention(q, *pool.args(), i32([[0]]), i32([5]), i32([0, 0]), 1, 64).shape == (4, 0, 64)
+    t = fastar.block_tables(i32([5, 0]), i32([0, 0]), 64, i32([1]), i32([0]), i32([[0], [1]]), 0)
+    assert t["cu"].tolist() == [0, 0, 0] and t["lens"].tolist() == [5, 0] and t["slots"].numel() == 0 and t["first"].tolist() == [0]
+    # sequences without new tokens beside one that has some
+    q = rows(gen(1), 4, 3, 64, torch.bfloat16)
+    out = torch.full_like(q, 2.0)
+    pool.fill(gen(2), i32([[0], [1]]), [64, 64])
+    fastar.kv8_attention(q, *pool.args(), i32([[0], [1]]), i32([60, 64]), i32([0, 0, 0]), 1, 64, out=out)
+    assert bool((out == 2.0).all())
+
+
 @pytest.mark.parametrize("n", [1, 4, 200])
 def test_paged_few_keys_in_a_large_bound(fastar, n):
     # the launch is sized for far more keys than there are
     paged(fastar, "bf16", 128, 4, 2, [n, n, n], [0, 3, 1300], extra_width=300, max_len=20000 - 800)
 
 
-@pytest.mark.parametrize("n", [1, 5, 140])
+@pytest.mark.parametrize("past", [300, 6000])                  # of one cluster's or item's keys, and cut into parts
+@pytest.mark.parametrize("n", [1, 5, 20, 140])
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64)])
-def test_paged_codes_that_are_not_seen_have_no_influence(fastar, n, dtype, D):
+def test_paged_codes_that_are_not_seen_have_no_influence(fastar, n, dtype, D, past):
     # NaN codes behind a row's own position (rows of the same call) reach only the rows that see them; bytes behind the end reach none
     def spoil(q, pool, table):
-        last = 300 + n - 1
+        last = past + n - 1
         page = int(table[1, last // 64])
         pool.codes[0][page, :, last % 64, 5] = 0x7F
         pool.codes[1][page, :, last % 64, 7] = 0xFF
-    paged(fastar, dtype, D, 4, 2, [n, n, n], [70, 300, 2], spoil=spoil)
+    paged(fastar, dtype, D, 4, 2, [n, n, n], [70, past, 2], spoil=spoil)
 
 
 @pytest.mark.parametrize("n", [1, 140])
