@@ -8,7 +8,7 @@
 // TMEM holds two S of 128 columns and two O of d.  At d = 128 that is all of it: P takes the place of its S, and a tile goes in two halves of 64 keys, so that the
 // products of one half run while the other is in its exponentials.  At d = 64 P lies beside, and Q K^T of the next tile follows as soon as the logits are in registers.
 // The running maximum is raised only when a logit exceeds it by 8 binary orders (O is rescaled then, by the warps that own its rows); sums add up the
-// probabilities as rounded.  Three of sixteen pairs of exponentials go to the FMA units.
+// probabilities as rounded.  Some of the exponentials go to the FMA units.
 // 8-bit cache: four warps read codes, two tiles ahead in registers, convert them to fp16 (exact) and put them where TMA would have put them.  Queries are fp16
 // too, their row divided by a power of two; a page's key scale goes into the factor of the logits, value scales are taken relative to the largest of the
 // CTA's keys (a power of two, so nothing is rounded within 2^15 of it; beyond that, and where there are NaN codes in a tile that some row does not see as a whole,
@@ -18,7 +18,7 @@
 // What bounds it: at d = 128 the card's power limit (990 W, 1.7 GHz of 1.965): tensor pipe 0.51 of the cycles packed, 0.40 with codes; exponentials 0.42 and 0.36.  At
 // d = 64 the soft-max warps' chain of load, maximum, exponentials, store.
 // Measured (B200, us): 16 384 tokens, 8 query and 2 key heads 515-530 (1.05 PFLOP/s); one warp issuing for both tiles, whole tiles of 128, 520-540; the same at d = 64
-// 396, whole tiles with P over S 445.  Three times 4 680 tokens, 12 heads, by frames 292-317.  1 560 queries over 29 640 8-bit keys, 12 heads 369-375: with the codes
+// 369, whole tiles with P over S 445.  Three times 4 680 tokens, 12 heads, by frames 292-317, at d = 64 231.  1 560 queries over 29 640 8-bit keys, 12 heads 369-375: with the codes
 // one tile ahead and NaN and scale work in every tile 614, whole tiles 455, queries by one warpgroup row by row and outputs by thread 396.  What an item costs beside its
 // tiles: some 5 000 cycles, 14 500 with queries and outputs that way (25 000 over codes).
 // Warp roles: 0-3 and 4-7 soft-max of the two tiles (and their queries and outputs), 8-11 the codes' way in (or the look at V), 12 and 13 MMAs of the two tiles, 14 K, 15 V (TMA).
@@ -45,7 +45,10 @@ __device__ __forceinline__ void set_regs() {
   else if constexpr (N < 128) setmaxnreg_dec<N>();
 }
 constexpr float kRaise = 8.f;
-constexpr int kPoly = 3;                                          // pairs of every 16 whose exponentials the FMA units work out
+// Pairs of every 16 whose exponentials the FMA units work out: the converting warps want their issue slots.  Packed, 16 384 tokens, d = 128, 2 / 3 / 4 / 5: 538 / 530 / 518 /
+// 527 us, d = 64 369 / 369 / 370 / 379; a frame over 8-bit keys 390 / 396 / 400 with 2 / 3 / 4 and 413 with 6.
+template <bool PAGED>
+constexpr int kPoly = PAGED ? 2 : 4;
 
 template <int D>
 struct ManySmem {
@@ -607,7 +610,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
         for (int e = 0; e < 32; ++e) {
           const uint32_t* y = &x[2 * h2 + (e >> 4)][2 * (e & 15)];
           const float2 u = ffma2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), ff, rr);
-          const float2 pr = e % 16 < kPoly ? poly_exp2(u) : make_float2(fast_exp2(u.x), fast_exp2(u.y));
+          const float2 pr = e % 16 < kPoly<PAGED> ? poly_exp2(u) : make_float2(fast_exp2(u.x), fast_exp2(u.y));
           p[e] = narrow2<M>(pr.x, pr.y);
           if (kHalf) add_f16x2(l[e & 1], p[e]);
           else add_bf16x2(l[e & 1], p[e]);
