@@ -11,8 +11,8 @@
 // probabilities as rounded.  Some of the exponentials go to the FMA units.
 // 8-bit cache: four warps read codes, two tiles ahead in registers, convert them to fp16 (exact) and put them where TMA would have put them.  Queries are fp16
 // too, their row divided by a power of two; a page's key scale goes into the factor of the logits, value scales are taken relative to the largest of the
-// CTA's keys (a power of two, so nothing is rounded within 2^15 of it; beyond that, and where there are NaN codes in a tile that some row does not see as a whole,
-// the rows are worked out from the definition).
+// CTA's keys (a power of two, so nothing is rounded within 2^15 of it, and a value by 2^-14 of its page's largest at most within 2^18; beyond that, and where there are NaN
+// codes in a tile that some row does not see as a whole, the rows are worked out from the definition).
 // What a row does not see must not reach it: V rows behind the last visible key are zeroed, and values that are not finite in a tile that some row does not see as
 // a whole are taken out, and all rows of the CTA are worked out from the definition afterwards (dense_rows.cuh).
 // What bounds it: at d = 128 the card's power limit (990 W, 1.7 GHz of 1.965): tensor pipe 0.51 of the cycles packed, 0.40 with codes; exponentials 0.42 and 0.36.  At
@@ -44,6 +44,7 @@ __device__ __forceinline__ void set_regs() {
   if constexpr (N > 128) setmaxnreg_inc<N>();
   else if constexpr (N < 128) setmaxnreg_dec<N>();
 }
+constexpr float kLeastShare = 3.8146973e-6f;                        // 2^-18: fp16 ends at 2^-24, a half of whose step is 2^-14.8 of the least such page's largest value
 constexpr float kRaise = 8.f;
 // Pairs of every 16 whose exponentials the FMA units work out: the converting warps want their issue slots.  Packed, 16 384 tokens, d = 128, 2 / 3 / 4 / 5: 538 / 530 / 518 /
 // 527 us, d = 64 369 / 369 / 370 / 379; a frame over 8-bit keys 390 / 396 / 400 with 2 / 3 / 4 and 413 with 6.
@@ -388,7 +389,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
         const uint32_t tile = sbase + (w.is_v ? SM::v_off : SM::k_off) + st * SM::q_tile;
         const float f0 = w.is_v ? w.scale.x / most : 1.f, f1 = w.is_v ? w.scale.y / most : 1.f;
         // (2^-126 is the scale of a page of zeros)
-        if ((f0 < 3.0517578e-5f && w.scale.x > 1.17549435e-38f) || (f1 < 3.0517578e-5f && w.scale.y > 1.17549435e-38f)) spoilt = true;
+        if ((f0 < kLeastShare && w.scale.x > 1.17549435e-38f) || (f1 < kLeastShare && w.scale.y > 1.17549435e-38f)) spoilt = true;
         const __half2 h0 = __float2half2_rn(f0), h1 = __float2half2_rn(f1);
         const int first = D == 128 ? c >> 2 : 0;                   // which of its two pieces a thread stores first: eight lanes, eight banks
         auto pass = [&](int p, auto look) {

@@ -321,6 +321,20 @@ def test_paged_scales_far_apart(fastar, n):
     paged(fastar, "bf16", 128, 4, 2, [n], [500], spoil=spoil)
 
 
+@pytest.mark.parametrize("n", [1, 140])
+@pytest.mark.parametrize("down", [-14, -17, -18, -19])
+def test_paged_scales_some_way_apart(fastar, n, down):
+    # a page whose values are up to 2^18 below the others', and further; the first queries see almost only that page
+    def spoil(q, pool, table):
+        q[:, : q.shape[1] // 2] = q[:, : q.shape[1] // 2].abs()
+        page = table[0, 2].long()
+        pool.codes[0][page] = pool.codes[0][page] & 0x7F
+        for p in (0, 1, 3):
+            pool.scale[1][table[0, p].long()] = 2.0 ** -6
+        pool.scale[1][page] = 2.0 ** (-6 + down)
+    paged(fastar, "bf16", 128, 2, 2, [n], [230], spoil=spoil, std=3.0)
+
+
 @pytest.mark.parametrize("n", [1, 3, 300])
 def test_paged_results_repeat_bit_for_bit(fastar, n):
     g = gen(9)
