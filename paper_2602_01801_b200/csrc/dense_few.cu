@@ -169,57 +169,72 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
     walk.x = item + static_cast<int64_t>(walk.f.tiles) * rank / share;
     walk.x_end = item + static_cast<int64_t>(walk.f.tiles) * (rank + 1) / share;
   } else {
-    {
-    int64_t* red = reinterpret_cast<int64_t*>(smem);
-    FewSeq f;
-    auto scan = [&](int b, int64_t& mine, int64_t& step) {         // units before sequence b of this step's, b's and the step's
-      mine = b < a.B ? few_seq(a, b, f) : 0;
-      int64_t x = mine;
+    if (a.B <= 32) {                                               // every warp by itself, a sequence a lane
+      FewSeq f;
+      const int64_t mine = lane < a.B ? few_seq(a, lane, f) : 0;
+      int64_t upto = mine;
 #pragma unroll
       for (int w = 1; w < 32; w <<= 1) {
-        const int64_t u = __shfl_up_sync(0xffffffffu, x, w);
-        if (lane >= w) x += u;
+        const int64_t u = __shfl_up_sync(0xffffffffu, upto, w);
+        if (lane >= w) upto += u;
       }
-      __syncthreads();
-      if (lane == 31) red[warp] = x;
-      __syncthreads();
-      int64_t off = 0;
-      step = 0;
+      units = __shfl_sync(0xffffffffu, upto, 31);
+      ctas = units < gridDim.x ? static_cast<int>(units) : gridDim.x;
+      if (static_cast<int>(blockIdx.x) >= ctas) return;
+      walk.x = few_first(units, blockIdx.x, ctas);
+      walk.b = __ffs(__ballot_sync(0xffffffffu, walk.x < upto)) - 1;
+      walk.base = __shfl_sync(0xffffffffu, upto - mine, walk.b);
+    } else {
+      int64_t* red = reinterpret_cast<int64_t*>(smem);
+      FewSeq f;
+      auto scan = [&](int b, int64_t& mine, int64_t& step) {         // units before sequence b of this step's, b's and the step's
+        mine = b < a.B ? few_seq(a, b, f) : 0;
+        int64_t x = mine;
 #pragma unroll
-      for (int w = 0; w < kFewThreads / 32; ++w) {
-        if (w < warp) off += red[w];
-        step += red[w];
+        for (int w = 1; w < 32; w <<= 1) {
+          const int64_t u = __shfl_up_sync(0xffffffffu, x, w);
+          if (lane >= w) x += u;
+        }
+        __syncthreads();
+        if (lane == 31) red[warp] = x;
+        __syncthreads();
+        int64_t off = 0;
+        step = 0;
+#pragma unroll
+        for (int w = 0; w < kFewThreads / 32; ++w) {
+          if (w < warp) off += red[w];
+          step += red[w];
+        }
+        return off + x - mine;
+      };
+      int64_t mine, step, before = scan(threadIdx.x, mine, step), all = step;
+      for (int b0 = kFewThreads; b0 < a.B; b0 += kFewThreads) {
+        int64_t unused;
+        scan(b0 + threadIdx.x, unused, step);
+        all += step;
       }
-      return off + x - mine;
-    };
-    int64_t mine, step, before = scan(threadIdx.x, mine, step), all = step;
-    for (int b0 = kFewThreads; b0 < a.B; b0 += kFewThreads) {
-      int64_t unused;
-      scan(b0 + threadIdx.x, unused, step);
-      all += step;
-    }
-    const int n = all < gridDim.x ? static_cast<int>(all) : gridDim.x;
-    if (static_cast<int>(blockIdx.x) >= n) return;
-    const int64_t first = few_first(all, blockIdx.x, n);
-    int64_t base = 0;
-    for (int b0 = 0;; b0 += kFewThreads) {                         // (the first step's sums are at hand)
-      if (b0 > 0 || a.B > kFewThreads) before = scan(b0 + threadIdx.x, mine, step);
-      else step = all;
-      if (mine > 0 && first >= base + before && first < base + before + mine) {
-        found_s[0] = all;
-        found_s[1] = base + before;
-        found_s[2] = b0 + threadIdx.x;
+      const int n = all < gridDim.x ? static_cast<int>(all) : gridDim.x;
+      if (static_cast<int>(blockIdx.x) >= n) return;
+      const int64_t first = few_first(all, blockIdx.x, n);
+      int64_t base = 0;
+      for (int b0 = 0;; b0 += kFewThreads) {                         // (the first step's sums are at hand)
+        if (b0 > 0 || a.B > kFewThreads) before = scan(b0 + threadIdx.x, mine, step);
+        else step = all;
+        if (mine > 0 && first >= base + before && first < base + before + mine) {
+          found_s[0] = all;
+          found_s[1] = base + before;
+          found_s[2] = b0 + threadIdx.x;
+        }
+        base += step;
+        if (base > first) break;
       }
-      base += step;
-      if (base > first) break;
+      __syncthreads();
+      units = found_s[0];
+      ctas = units < gridDim.x ? static_cast<int>(units) : gridDim.x;
+      walk.b = static_cast<int>(found_s[2]);
+      walk.base = found_s[1];
+      walk.x = few_first(units, blockIdx.x, ctas);
     }
-    __syncthreads();
-    }
-    units = found_s[0];
-    ctas = units < gridDim.x ? static_cast<int>(units) : gridDim.x;
-    walk.b = static_cast<int>(found_s[2]);
-    walk.base = found_s[1];
-    walk.x = few_first(units, blockIdx.x, ctas);
     walk.x_end = few_first(units, blockIdx.x + 1, ctas);
     few_seq(a, walk.b, walk.f);
   }

@@ -131,20 +131,36 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   chain_wait();
 
   // ---- the item: tiles of the sequences in order, a sequence's last (longest) first
-  {
+  ManyItem it;
+  DenseSeq s{0, 0, 0};
+  int item_tile = 0;
+  auto tiles_of = [&](int b, DenseSeq& found) {
+    const int r = seq_of(a, b, found);
+    if (r < 0 && a.status) record_status(a.status, kErrBounds);
+    const int rows = found.n * a.G;
+    return r > 0 && rows > a.few_rows ? (rows + kRowsCta - 1) / kRowsCta : 0;
+  };
+  if (a.B <= 32) {                                                 // every warp by itself, a sequence a lane
+    const int tile = blockIdx.x / a.KV, mine = lane < a.B ? tiles_of(lane, s) : 0;
+    int64_t upto = mine;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+      const int64_t u = __shfl_up_sync(0xffffffffu, upto, w);
+      if (lane >= w) upto += u;
+    }
+    const unsigned has = __ballot_sync(0xffffffffu, tile < upto);  // the first of these lanes' sequence, if any
+    const int b = has ? __ffs(has) - 1 : 0;
+    it.b = has ? b : -1;
+    item_tile = static_cast<int>(__shfl_sync(0xffffffffu, upto, b)) - 1 - tile;
+    s = DenseSeq{__shfl_sync(0xffffffffu, s.t0, b), __shfl_sync(0xffffffffu, s.n, b), __shfl_sync(0xffffffffu, s.len, b)};
+    __syncthreads();
+  } else {
     int* red = reinterpret_cast<int*>(smem);                       // 17 words
     const int tile = blockIdx.x / a.KV;
     int64_t before = 0;
     for (int b0 = 0; b0 < a.B && before <= tile; b0 += kManyThreads) {
       const int b = b0 + threadIdx.x;
-      int mine = 0;
-      DenseSeq s;
-      if (b < a.B) {
-        const int r = seq_of(a, b, s);
-        if (r < 0 && a.status) record_status(a.status, kErrBounds);
-        const int rows = s.n * a.G;
-        if (r > 0 && rows > a.few_rows) mine = (rows + kRowsCta - 1) / kRowsCta;
-      }
+      const int mine = b < a.B ? tiles_of(b, s) : 0;
       int x = mine;
 #pragma unroll
       for (int w = 1; w < 32; w <<= 1) {
@@ -170,13 +186,13 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       before += all;
       __syncthreads();
     }
+    it.b = item_s[0];
+    item_tile = item_s[1];
+    s = DenseSeq{item_s[2], item_s[3], item_s[4]};
   }
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   chain_next();
-  ManyItem it;
-  it.b = item_s[0];
-  const DenseSeq s{item_s[2], item_s[3], item_s[4]};
   it.kvh = blockIdx.x % a.KV;
   it.part = blockIdx.y;
   const bool whole = !PAGED || a.parts == 1 || s.len <= a.chunk;     // (packed: the keys are never cut)
@@ -185,7 +201,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
     return;
   }
   it.rows = s.n * a.G;
-  it.row0 = item_s[1] * kRowsCta;
+  it.row0 = item_tile * kRowsCta;
   it.past = s.len - s.n;
   it.k0 = whole ? 0 : it.part * a.chunk;
   it.see = 0;
