@@ -50,7 +50,8 @@ extern "C" {
 #define FASTAR_ERR_TIMEOUT            -5   /* a bounded device-side wait gave up */
 #define FASTAR_ERR_NOT_SM100          -6
 #define FASTAR_ERR_WORKSPACE          -7   /* workspace buffer too small or misaligned */
-#define FASTAR_ERR_BOUNDS             -8   /* range-checking build only: a computed index left its array (access redirected) */
+#define FASTAR_ERR_BOUNDS             -8   /* an index left its array, access redirected or passed over: a computed one (range-checking build), or one of
+                                            * the tables and lengths that the dense path is given (every build) */
 
 typedef struct fastar_cache fastar_cache_t;          /* opaque host object */
 

@@ -1212,7 +1212,7 @@ const char* fastar_status_string(int status) {
     case FASTAR_ERR_TIMEOUT: return "a bounded device-side wait gave up";
     case FASTAR_ERR_NOT_SM100: return "device is not compute capability 10.x";
     case FASTAR_ERR_WORKSPACE: return "workspace too small or misaligned";
-    case FASTAR_ERR_BOUNDS: return "range-checking build: a computed index left its array";
+    case FASTAR_ERR_BOUNDS: return "an index left its array: a computed one (range-checking build), or a length or page that the dense path was given";
     default: return "unknown status";
   }
 }
