@@ -274,6 +274,28 @@ def test_packed_many_sequences(fastar):
     packed(fastar, "bf16", 64, 2, 1, [(7 * b) % 6 for b in range(700)] + [300], 1)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,KV", [(64, 1), (130, 1), (96, 2)])
+def test_paged_wide_groups(fastar, D, H, KV):
+    # more query heads to a key head than the kernel for few rows has rows, and than a query tile has
+    paged(fastar, "bf16", D, H, KV, [1, 3, 1], [500, 40, 2000], 64)
+
+
+def test_packed_wide_groups(fastar):
+    packed(fastar, "bf16", 128, 130, 1, [5, 1, 40], 1)
+    packed(fastar, "fp16", 64, 96, 2, [5, 1, 40], 3)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_that_are_no_numbers_stay_by_themselves(fastar, D):
+    def bad_rows(q, *_):
+        q[0, 3], q[1, 5, 7], q[1, 60] = float("nan"), float("nan"), float("nan")
+    packed(fastar, "bf16", D, 2, 1, [70, 40], 1, spoil=lambda q, k, v, cu: bad_rows(q))
+    packed(fastar, "fp16", D, 2, 2, [70, 40], 0, spoil=lambda q, k, v, cu: bad_rows(q))
+    paged(fastar, "bf16", D, 2, 1, [70, 40], [300, 0], spoil=bad_rows)
+    paged(fastar, "fp16", D, 2, 1, [7, 7], [300, 6000], spoil=lambda q, *_: q[0, 3].fill_(float("nan")))
+
+
 def test_nothing_to_do(fastar):
     q = torch.zeros(4, 0, 64, dtype=torch.bfloat16, device=DEV)
     pool = Pool(2, 2, 64, 64)
