@@ -455,18 +455,14 @@ def _refuse(where: str):
 
 
 def _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale) -> bool:
-    P, KV = k_codes.shape[0], k_codes.shape[1]
-    u8, f32 = torch.uint8, torch.float32
+    u8, f32, codes, scales = torch.uint8, torch.float32, k_codes.shape, k_scale.shape
     return (k_codes.dtype == u8 and v_codes.dtype == u8 and k_scale.dtype == f32 and v_scale.dtype == f32 and k_codes.get_device() == dev and v_codes.get_device() == dev
             and k_scale.get_device() == dev and v_scale.get_device() == dev and k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
-            and v_scale.is_contiguous() and v_codes.shape == k_codes.shape and k_scale.shape == (P, KV) and v_scale.shape == (P, KV))
+            and v_scale.is_contiguous() and v_codes.shape == codes and v_scale.shape == scales and scales == codes[:2])
 
 
-def _ints_ok(i32, dev, *tensors) -> bool:
-    for t in tensors:
-        if t.dtype != i32 or t.get_device() != dev or not t.is_contiguous():
-            return False
-    return True
+def _int_ok(i32, dev, t) -> bool:
+    return t.dtype == i32 and t.get_device() == dev and t.is_contiguous()
 
 
 def _out_like(torch, q, strides, out, where):
@@ -485,7 +481,7 @@ def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add:
     where, dev = "block_tables", held.get_device()
     if not (dev >= 0 and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and free_pages.dim() == 1
             and first.numel() == 1 and max_add >= 0
-            and _ints_ok(i32, dev, held, add, free_pages, first, table)):
+            and _int_ok(i32, dev, held) and _int_ok(i32, dev, add) and _int_ok(i32, dev, free_pages) and _int_ok(i32, dev, first) and _int_ok(i32, dev, table)):
         _refuse(where)
     if dev != current():
         with torch.cuda.device(dev):
@@ -508,7 +504,8 @@ def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu
             and v_new.get_device() == dev and k_codes.dim() == 4 and _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale)):
         _refuse(where)
     (P, KV, PT, D), B = k_codes.shape, lens.shape[0]
-    if not (shape[0] == KV and shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and cu.shape == (B + 1,) and _ints_ok(i32, dev, table, lens, cu)):
+    if not (shape[0] == KV and shape[2] == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and cu.shape == (B + 1,)
+            and _int_ok(i32, dev, table) and _int_ok(i32, dev, lens) and _int_ok(i32, dev, cu)):
         _refuse(where)
     if dev != current():
         with torch.cuda.device(dev):
@@ -527,7 +524,8 @@ def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_ne
     if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and k_codes.dim() == 4 and _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale)):
         _refuse(where)
     (P, KV, PT, D), (H, T, d), B = k_codes.shape, shape, lens.shape[0]
-    if not (d == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and cu.shape == (B + 1,) and _ints_ok(i32, dev, table, lens, cu)):
+    if not (d == D and table.dim() == 2 and table.shape[0] == B and lens.dim() == 1 and cu.shape == (B + 1,)
+            and _int_ok(i32, dev, table) and _int_ok(i32, dev, lens) and _int_ok(i32, dev, cu)):
         _refuse(where)
     if dev != current():
         with torch.cuda.device(dev):
@@ -551,7 +549,7 @@ def packed_attention(q, k, v, cu, max_tokens: int, frame_len: int = 1, out=None)
     dtype, shape, strides, kv_shape, kv_strides = dtypes.get(q.dtype), q.shape, q.stride(), k.shape, k.stride()
     if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and len(kv_shape) == 3 and kv_strides[2] == 1 and k.dtype == q.dtype and v.dtype == q.dtype
             and v.shape == kv_shape and v.stride() == kv_strides and k.get_device() == dev and v.get_device() == dev and kv_shape[1:] == shape[1:]
-            and cu.dim() == 1 and cu.shape[0] >= 2 and _ints_ok(i32, dev, cu)):
+            and cu.dim() == 1 and cu.shape[0] >= 2 and _int_ok(i32, dev, cu)):
         _refuse(where)
     if dev != current():
         with torch.cuda.device(dev):
