@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
           float v = fmaxf(x[0][n][h], x[0][n][2 + h]);
 #pragma unroll
           for (int mt = 1; mt < MT; ++mt) v = fmax3(v, x[mt][n][h], x[mt][n][2 + h]);
-          mx[n][h] = v * (factor[n][h] * k_scale);
+          mx[n][h] = v * logit_factor(factor[n][h], k_scale);
           change |= mx[n][h] > m[n][h] + kFewRaise;
         }
       if (__any_sync(0xffffffffu, change)) {
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
       uint32_t p[MT][NR][2];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        const float2 f = make_float2(factor[n][0] * k_scale, factor[n][1] * k_scale);
+        const float2 f = make_float2(logit_factor(factor[n][0], k_scale), logit_factor(factor[n][1], k_scale));
         const float2 ref = make_float2(m[n][0] == -INFINITY ? 0.f : -m[n][0], m[n][1] == -INFINITY ? 0.f : -m[n][1]);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)

@@ -555,8 +555,8 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       if (PAGED) {
         float2 ks;
         asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks.x), "=f"(ks.y) : "r"(sbase + SM::scale_off + (j & 7) * 8));
-        f[0] = factor * (a.PT == 64 && NS == 2 && h == 1 ? ks.y : ks.x);
-        f[1] = factor * (a.PT == 64 ? ks.y : ks.x);
+        f[0] = logit_factor(factor, a.PT == 64 && NS == 2 && h == 1 ? ks.y : ks.x);
+        f[1] = logit_factor(factor, a.PT == 64 ? ks.y : ks.x);
       }
       tmem_wait_ld();
       if (!kOver) {

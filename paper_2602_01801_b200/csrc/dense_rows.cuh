@@ -37,6 +37,11 @@ __device__ __forceinline__ void add_f16x2(float2& s, uint32_t b) {
   asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.f16 %0, l, %0; add.f32.f16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
 }
 
+// What a logit is multiplied by: the power of two that its query row was divided by, 1 / sqrt(d), and the scale of its key's page.  The product of queries below 2^-20 and
+// a page of zero keys (scale 2^-126) would round to 0, and that of large ones overflow: kept positive and finite, -inf stays what it is where a key is not seen, and a
+// logit of 0 too.  Logits that the lower end scales are below 2^-100 either way.
+__device__ __forceinline__ float logit_factor(float row, float page) { return fminf(fmaxf(row * page, 1.17549435e-38f), 3.4028235e38f); }
+
 // D / 32 neighbouring columns of a row a lane.
 template <class T, int D>
 __device__ __forceinline__ void load_cols(const T* row, int lane, float (&x)[D / 32]) {

@@ -1,0 +1,50 @@
+"""The dense path at the ends of what scales, queries and weights may be."""
+import pytest
+import torch
+
+from tests import test_gpu_dense as base
+from tests.test_gpu_dense import clean_status, fastar  # noqa: F401  (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------- key scales far below and far above the queries
+def zero_key_pages(*which):
+    def spoil(q, pool, table):
+        for b, i in which:
+            page = table[b, i].long()
+            pool.codes[0][page] = 0
+            pool.scale[0][page] = 2.0 ** -126
+    return spoil
+
+
+@pytest.mark.parametrize("tiny", [1e-7, 1e-20, 1e-37])
+@pytest.mark.parametrize("n", [1, 5, 140])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("fp16", 128)])
+def test_zero_keys_and_small_queries(fastar, tiny, n, dtype, D):  # noqa: F811
+    """Pages of zero keys have the least scale, 2^-126.  With queries that are small too their product leaves fp32, and keys that a row does not see must stay
+    out all the same: what is seen has equal weights."""
+    if dtype == "fp16" and tiny < 1e-7:
+        tiny = 6e-8                                                             # the least number of the type
+    base.paged(fastar, dtype, D, 4, 2, [n, n], [500, 37], std=tiny, spoil=zero_key_pages((0, 0), (0, (500 + n - 1) // 64), (1, 0), (1, (37 + n - 1) // 64)))
+
+
+@pytest.mark.parametrize("past", [3, 6001])                    # an item of a cluster, and cut ones
+@pytest.mark.parametrize("n", [1, 140])
+def test_all_keys_zero(fastar, past, n):  # noqa: F811
+    pages = range(-(-(past + n) // 64))
+    base.paged(fastar, "bf16", 128, 2, 1, [n], [past], std=1e-7, spoil=zero_key_pages(*((0, i) for i in pages)))
+
+
+@pytest.mark.parametrize("n", [1, 5, 140])
+def test_large_queries_and_key_scales(fastar, n):  # noqa: F811
+    """Zero codes in a page whose scale times the queries' leaves fp32 at the other end: their logits are 0 all the same."""
+    def spoil(q, pool, table):
+        for i in (0, 2):
+            page = table[0, i].long()
+            pool.codes[0][page] = 0
+            pool.scale[0][page] = 2.0 ** 100
+        for i in range(1, -(-(230 + n) // 64)):
+            if i != 2:
+                pool.scale[0][table[0, i].long()] = 2.0 ** -100                 # logits of up to some 2^12
+    base.paged(fastar, "bf16", 128, 4, 2, [n], [230], std=2.0 ** 100, spoil=spoil)
