@@ -600,14 +600,13 @@ template <class T, int D, int WARPS>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
   __shared__ float o_s[WARPS][D];
   __shared__ float2 ml_s[WARPS];
-  // (cu and lens are there before chain_wait: the kernel before this one lets it start only once it has waited for those before itself, and writes neither)
   const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : warp_index();
   const int64_t row = WARPS == 1 ? static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + warp_index() : blockIdx.x;
   if (row >= static_cast<int64_t>(a.T) * a.H) return;              // (a whole CTA, or a warp of its own)
+  chain_wait();                                                    // for cu and lens too: only this makes what was written before visible here
   const int t = static_cast<int>(row / a.H), head = static_cast<int>(row - static_cast<int64_t>(t) * a.H), b = seq_of_token(a, t);
   DenseSeq s;
   const int found = seq_of(a, b, s);
-  chain_wait();
   if (found <= 0 || t < s.t0 || t >= s.t0 + s.n) return;
   const bool few = s.n * a.G <= a.few_rows;
   int parts, first = 0, row_of_few = 0;

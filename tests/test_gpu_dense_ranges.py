@@ -48,3 +48,48 @@ def test_large_queries_and_key_scales(fastar, n):  # noqa: F811
             if i != 2:
                 pool.scale[0][table[0, i].long()] = 2.0 ** -100                 # logits of up to some 2^12
     base.paged(fastar, "bf16", 128, 4, 2, [n], [230], std=2.0 ** 100, spoil=spoil)
+
+
+# ------------------------------------------------------------------------------------- calls that follow on one another without a pause
+@pytest.mark.parametrize("most", [3, 140])                     # new tokens: cut items of few rows, parts of many
+def test_lengths_that_change_from_call_to_call(fastar, most):  # noqa: F811
+    """Steps whose tables, attention and join run straight after one another, with lengths and prefix sums written where those of the step before lay: the
+    bits of the same calls with the GPU idle in between."""
+    g = base.gen(31)
+    H, KV, D, PT, B, W, steps = 4, 2, 128, 64, 3, 130, 6
+    pool = base.Pool(B * W, KV, PT, D)
+    free = torch.randperm(B * W, generator=g, device=base.DEV).to(torch.int32)
+    pool.fill(g, torch.arange(B * W, dtype=torch.int32, device=base.DEV).view(1, -1), [B * W * PT])
+    adds = [base.i32([(i * 7 + 3 * s * s) % (most + 1) for i in range(B)]) for s in range(steps)]
+    T = B * most
+    qs = [base.rows(g, H, T, D, torch.bfloat16) for _ in range(steps)]
+    held, first = torch.zeros(B, dtype=torch.int32, device=base.DEV), base.i32([0])
+    zeros, empty = base.i32([0] * B), torch.full((B, W), -1, dtype=torch.int32, device=base.DEV)
+
+    def run(outs, pause):
+        table, h = empty.clone(), held
+        f = fastar.block_tables(zeros, h, PT, free, first, table, 3 * 8000)["first"]
+        for s in range(steps):
+            t = fastar.block_tables(h, adds[s], PT, free, f, table, T)
+            pause()
+            fastar.kv8_attention(qs[s], *pool.args(), table, t["lens"], t["cu"], most, W * PT, out=outs[s])
+            pause()
+            h, f = t["lens"], t["first"]
+
+    want, got = ([torch.zeros_like(q) for q in qs] for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    run(got, lambda: None)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        run(got, lambda: None)
+    for lens in ([5000, 1, 7000], [64, 6400, 3001], [0, 0, 7300], [7000, 5000, 127]):
+        held.copy_(base.i32(lens))
+        for o in (*want, *got):
+            o.zero_()
+        torch.cuda.synchronize()
+        run(want, torch.cuda.synchronize)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
+        assert any(bool(w.any()) for w in want)
