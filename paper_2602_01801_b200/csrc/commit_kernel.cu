@@ -63,8 +63,8 @@ __device__ __forceinline__ void store_code_part(const CacheView& c, int page, in
 constexpr int kCommitThreads = 64;
 
 template <int D, bool MEANK>
-__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CacheView c, const __nv_bfloat16* __restrict__ k_new,
-                                                     const __nv_bfloat16* __restrict__ v_new, int n, int frame_len, int64_t hs,
+__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CacheView c, const __nv_bfloat16* k_new,
+                                                     const __nv_bfloat16* v_new, int n, int frame_len, int64_t hs,
                                                      int64_t ts) {
   chain_wait();
   constexpr int LPR = D / 8;            // lanes per row

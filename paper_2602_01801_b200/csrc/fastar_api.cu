@@ -288,7 +288,7 @@ int make_range(fastar_cache* c, int h0, int count, HeadRange* out) {
 }
 
 // Block scores of weighted histograms as one number: lo + 256 * hi (exact in fp32 below 2^24).
-__global__ void combine_scores_kernel(const float* __restrict__ lo, const float* __restrict__ hi, int64_t head_stride,
+__global__ void combine_scores_kernel(const float* lo, const float* hi, int64_t head_stride,
                                       float* __restrict__ out, int per_head) {
   chain_wait();
   const int h = blockIdx.y;
@@ -296,7 +296,7 @@ __global__ void combine_scores_kernel(const float* __restrict__ lo, const float*
     out[static_cast<int64_t>(h) * per_head + q] = lo[h * head_stride + q] + 256.f * hi[h * head_stride + q];
 }
 
-__global__ void copy_rows3_kernel(const int32_t* __restrict__ src, int64_t src_hs, int src_rs, int32_t* __restrict__ dst, int rows,
+__global__ void copy_rows3_kernel(const int32_t* src, int64_t src_hs, int src_rs, int32_t* __restrict__ dst, int rows,
                                   int cols) {
   chain_wait();
   const int h = blockIdx.y;

@@ -42,8 +42,9 @@ __device__ __forceinline__ int checked_index(int idx, int n, int* status) {
 // memory that another kernel reads or writes.
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// The grid behind may become resident from here on (it still waits in its chain_wait for all of this one).  What it reads may be written while it is resident, so it
-// reads nothing by the path for data that a kernel never sees change (__ldg, const __restrict__).
+// The grid behind may become resident from here on (it still waits in its chain_wait for all of this one).  What it reads may be written while it is resident, so no
+// kernel that is launched by launch_chained reads by the path for data that a kernel never sees change: no __ldg, and no input that is const and __restrict__
+// (tests/test_chained_kernels_cpu.py).  Without it hashing, commit and quantising take as long as with it.
 __device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // What this thread, and the threads that a barrier has ordered before it, wrote is seen by whoever reads a later count.

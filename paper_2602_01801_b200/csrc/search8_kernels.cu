@@ -91,7 +91,7 @@ int launch_quantize_rows(const CacheView& c, const QuantizeRows& a, const Quanti
 // 0xB8), zero padded to 128 bytes, so that the dot product of two rows is T*b - 2 * (Hamming distance) and the
 // arg-max of the search kernel is the key at the smallest Hamming distance (ties -> lowest slot).  One thread per 8
 // bytes; bit u of table t sits at bit 8*t + u of the packed code.
-__global__ void __launch_bounds__(256) sign_rows_kernel(const uint32_t* __restrict__ codes, int H, int n, int64_t code_stride, int T,
+__global__ void __launch_bounds__(256) sign_rows_kernel(const uint32_t* codes, int H, int n, int64_t code_stride, int T,
                                                         int B, uint8_t* __restrict__ out, int64_t out_rows_per_head) {
   chain_wait();
   const int64_t total = static_cast<int64_t>(H) * n * 16;
@@ -124,8 +124,8 @@ int launch_sign_rows(const CacheView& c, const uint32_t* codes, int n, int64_t c
 }
 
 // One thread per 8 components of a 128-byte code row.
-__global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* __restrict__ x, int H, int n, int D, int64_t hs,
-                                                       int64_t ts, const float* __restrict__ rnorm, int64_t rn_stride,
+__global__ void __launch_bounds__(256) quantize_kernel(const __nv_bfloat16* x, int H, int n, int D, int64_t hs,
+                                                       int64_t ts, const float* rnorm, int64_t rn_stride,
                                                        uint8_t* __restrict__ out, int64_t out_rows_per_head) {
   chain_wait();
   const int64_t total = static_cast<int64_t>(H) * n * 16;

@@ -146,8 +146,8 @@ struct BlockHist {
   int max_qb, hist_cols;
 };
 template <int D, int ROWS, bool F32>
-__global__ void __launch_bounds__(256, 2) prep_kernel(const __nv_bfloat16* __restrict__ x, int H, int n, int64_t hs, int64_t ts,
-                                                   const __nv_bfloat16* __restrict__ lsh, int T, int B,
+__global__ void __launch_bounds__(256, 2) prep_kernel(const __nv_bfloat16* x, int H, int n, int64_t hs, int64_t ts,
+                                                   const __nv_bfloat16* lsh, int T, int B,
                                                    uint32_t* __restrict__ code_out, float* __restrict__ rnorm_out,
                                                    int64_t out_stride, UpdateScratch clear, BlockHist bh, const ConvertArgs conv) {
   constexpr bool BLOCKS = ROWS > 0;
@@ -872,7 +872,7 @@ __global__ void __launch_bounds__(256) scatter_kernel(const CacheView c, int n, 
 // key similarity, so the packed word of token i becomes (cos(k_i, k_j*), j*) with the cosine in the same fp32
 // form as the cosine search (dot * 1/|k_i| * 1/|k_j*|).  Half a warp per token, one 128-bit load per lane and row.
 // ---------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) probe_cosine_kernel(const CacheView c, const __nv_bfloat16* __restrict__ k_new, int n,
+__global__ void __launch_bounds__(256) probe_cosine_kernel(const CacheView c, const __nv_bfloat16* k_new, int n,
                                                            int64_t hs, int64_t ts) {
   chain_wait();
   const int64_t rows = static_cast<int64_t>(c.H) * n;

@@ -37,3 +37,18 @@ def test_nothing_is_read_before_the_kernel_in_front_is_through(kernel):
     """chain_wait makes the writes of the kernels in front visible; a kernel in front that lets this one start earlier does not."""
     before = kernel[2][: kernel[2].index("chain_wait()")]
     assert not READS.search(before), READS.search(before).group(0)
+
+
+def test_no_input_of_a_chained_kernel_is_taken_for_constant():
+    """A pointer that is const and __restrict__ lets the compiler load by the path for data that nobody writes while the kernel is resident.  The kernel in front, which
+    may let this one become resident early (chain_next), does write: its output is this one's input."""
+    for name, head, body in kernels():
+        if "chain_wait()" in body:
+            assert not re.search(r"\bconst\s+[\w:]+\s*\*\s*(const\s+)?__restrict__|[\w:]+\s+const\s*\*\s*__restrict__", head), (name, head)
+    for name in sorted(os.listdir(CSRC)):
+        if name.endswith((".cu", ".cuh", ".h")):
+            with open(os.path.join(CSRC, name)) as f:
+                text = re.sub(r"//[^\n]*", "", f.read())
+            assert not re.search(r"\b__ldg\s*\(|ld\.global(\.\w+)*\.nc\b", text), name
+            if name.endswith((".cuh", ".h")):
+                assert not re.search(r"\bconst\s+[\w:]+\s*\*\s*(const\s+)?__restrict__", text), name

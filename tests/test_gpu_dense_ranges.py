@@ -93,3 +93,49 @@ def test_lengths_that_change_from_call_to_call(fastar, most):  # noqa: F811
         for a, b in zip(want, got):
             assert torch.equal(a, b)
         assert any(bool(w.any()) for w in want)
+
+
+@pytest.mark.parametrize("search_bits", [16, 8, 1])
+@pytest.mark.parametrize("probe", [False, True])
+def test_outputs_straight_into_the_sparse_step(fastar, search_bits, probe):  # noqa: F811
+    """What dense attention writes is the very next kernel's input, in a cache's update and in its attention: the bits of the same calls with the GPU idle
+    in between."""
+    if probe and search_bits == 1:
+        pytest.skip("sign bits have no dot products for the probe")
+    import numpy as np
+    g = base.gen(41)
+    H, D, n = 3, 128, 520
+    lsh = np.random.default_rng(5).standard_normal((32, D)).astype(np.float32)
+    q, k, v = (base.rows(g, H, n, D, torch.bfloat16) for _ in range(3))
+    cu, kp = base.i32([0, n]), base.rows(g, H, 48, D, torch.bfloat16)
+
+    def run(pause):
+        cache = fastar.Cache(H, D, 4096, 64, lsh, max_tokens=2 * n, max_prompt_tokens=48, max_frames=2, search_bits=search_bits)
+        cache.update(k, v, n, 2.0, outputs=False)
+        a, b, c = (torch.zeros_like(q) for _ in range(3))
+        found = []
+        for i in range(6):
+            fastar.packed_attention(q, k, v, cu, n, frame_len=1 + i, out=a)
+            fastar.packed_attention(k, q, v, cu, n, frame_len=3 + i, out=b)
+            fastar.packed_attention(v, k, q, cu, n, frame_len=1 + i, out=c)
+            pause()
+            found.append(cache.update(c, b, n, 0.9, probe=a if probe else None))
+            pause()
+            fastar.packed_attention(b, q, v, cu, n, frame_len=2 + i, out=a)
+            pause()
+            found.append(cache.annsa(a, 64, 5))
+            pause()
+            fastar.packed_attention(k, b, q, cu, n, frame_len=2 + i, out=a)
+            pause()
+            found.append(cache.annca(a, kp, kp, n, 8))
+            pause()
+        torch.cuda.synchronize()
+        assert cache.status() == fastar.OK
+        return found
+
+    want = run(torch.cuda.synchronize)
+    for _ in range(3):
+        for x, y in zip(want, run(lambda: None)):
+            assert x.keys() == y.keys()
+            for name in x:
+                assert torch.equal(x[name], y[name]), name
