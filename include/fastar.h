@@ -385,8 +385,8 @@ int fastar_noalloc_last_status(void* stream);
  * [i page_tokens, (i+1) page_tokens) of the sequence.  All contiguous.  page_tokens: 64 or 128; d: 64 or 128.
  * dtype: FASTAR_BF16 or FASTAR_FP16, of q, k, v and out; fp32 accumulation and soft-max.  num_heads is a multiple of num_kv_heads;
  * query head h reads key head h / (num_heads / num_kv_heads).  Strides as elsewhere (one over a single head or token is not used); rows
- * do not overlap, and out is no input.  Scales are powers of two, as fastar_kv8_append writes them.  1 <= num_seqs <= 2^20; T x num_heads and
- * max_len are at most 2^30.
+ * do not overlap, and out is no input.  Scales are powers of two, as fastar_kv8_append writes them.  1 <= num_seqs <= 2^20; T x num_heads,
+ * max_len and max_add are at most 2^30.
  * Frames: a token sees the keys of its sequence up to the end of its own frame of frame_len tokens (positions
  * [0, (floor(position / frame_len) + 1) frame_len)), frame_len = 1 being the causal mask; 0: all keys of the sequence.
  * What is not seen has no influence, whatever its bits are.  A row that sees only logits of -inf gives zeros.

@@ -58,8 +58,9 @@ int shape_ok(int H, int KV, int D, int dtype) {
 // Rows and positions are counted in 32 bits.
 constexpr int64_t kMostRows = int64_t{1} << 30;
 bool too_long(int total, int max_len, int H) { return static_cast<int64_t>(total) * H > kMostRows || max_len > kMostRows; }
+constexpr int kMostSeqs = 1 << 20;
 // ... and shares of all tiles in 64: sequences x key heads x tiles x CTAs
-bool too_many(int seqs, int max_len, int KV) { return seqs > (1 << 20) || static_cast<int64_t>(seqs) * KV * (max_len / kFewKeys + 1) > (int64_t{1} << 50); }
+bool too_many(int seqs, int max_len, int KV) { return seqs > kMostSeqs || static_cast<int64_t>(seqs) * KV * (max_len / kFewKeys + 1) > (int64_t{1} << 50); }
 // Tiles of 128 tokens x 64 columns of a packed tensor [heads][T][d].
 int encode_packed(CUtensorMap* m, const void* ptr, int d, int64_t tokens, int heads, int64_t ts, int64_t hs, bool fp16) {
   if (tokens == 1) ts = d;                                         // (a stride over one token or one head is not used)
@@ -146,7 +147,7 @@ extern "C" int fastar_block_tables(const int32_t* held, const int32_t* add, int3
                                    int64_t* slots, int32_t max_add, int32_t* first_out, void* stream) {
   if (!held || !add || !free_pages || !first || !table || !cu || !lens || !first_out || (!slots && max_add > 0)) return FASTAR_ERR_INVALID_ARG;
   if (num_seqs < 1 || num_free < 0 || table_width < 1 || max_add < 0 || first == first_out || held == lens || add == lens) return FASTAR_ERR_INVALID_ARG;
-  if (page_tokens != 64 && page_tokens != 128) return FASTAR_ERR_UNSUPPORTED_SHAPE;
+  if ((page_tokens != 64 && page_tokens != 128) || num_seqs > kMostSeqs || max_add > kMostRows) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (!aligned(held, 4) || !aligned(add, 4) || !aligned(free_pages, 4) || !aligned(first, 4) || !aligned(table, 4) || !aligned(cu, 4) || !aligned(lens, 4) ||
       !aligned(slots, 8) || !aligned(first_out, 4))
     return FASTAR_ERR_INVALID_ARG;

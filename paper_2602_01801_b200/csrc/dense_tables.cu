@@ -39,7 +39,8 @@ __device__ __forceinline__ void block_scan2(int64_t& x, int64_t& y, int64_t& all
 // need_b = pages(held + add) - pages(held); the requests' needs and tokens are summed up in order, and request b gets the free pages from its
 // predecessors' sum on.  Every CTA sums up all requests by itself (1024 a step, 8 bytes each, out of L2 but for the first), so that none waits for
 // another, and writes its share of the tokens' slots and of the new table entries, for which it looks up the request by bisection.  What bounds it
-// is the chain of three loads, two sums and ten steps of bisection.
+// is the chain of three loads, two sums and ten steps of bisection.  Slots and requests are counted in 32 bits: 2^30 of the former at most, so that a grid's
+// step behind the last is one too.
 constexpr int kTableThreads = 1024;
 
 struct TableReq {
@@ -109,7 +110,7 @@ block_tables_kernel(const int32_t* held, const int32_t* add, int B, int PT, cons
       const TableReq r = req[lo];
       int64_t slot = -1;
       if (r.need >= 0) {
-        const int pos = r.held + t - r.cu, i = pos / PT, before = pages_of(r.held, PT);
+        const int pos = r.held + (t - r.cu), i = pos / PT, before = pages_of(r.held, PT);
         const int page = i < before ? table[static_cast<int64_t>(b0 + lo) * W + i] : free_pages[f0 + r.upto + i - before];
         if (page >= 0) slot = static_cast<int64_t>(page) * PT + pos % PT;
       }

@@ -92,6 +92,12 @@ def test_table_refusals(lib, mem, bad, status):
     assert lib.fastar_block_tables(*table_args(p, slots=p + 4)) == -1
 
 
+@pytest.mark.parametrize("bad", [dict(max_add=2 ** 30 + 1), dict(max_add=2 ** 31 - 1), dict(seqs=2 ** 20 + 1), dict(seqs=2 ** 31 - 1)])
+def test_table_limits(lib, mem, bad):
+    """Slots and requests are counted in 32 bits, with room for a grid's step: as many as the other calls take."""
+    assert lib.fastar_block_tables(*table_args(mem[0], cu=mem[0] + 192, **bad)) == -2
+
+
 def test_arguments_as_words(lib, mem):
     """fastar_dense_call takes the calls' arguments as 64-bit words and answers as they do; a count or a 32-bit argument that is not theirs is refused."""
     from paper_2602_01801_b200 import fastar
