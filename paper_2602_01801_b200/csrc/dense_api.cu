@@ -145,7 +145,7 @@ using namespace fastar;
 extern "C" int fastar_block_tables(const int32_t* held, const int32_t* add, int32_t num_seqs, int32_t page_tokens, const int32_t* free_pages,
                                    int32_t num_free, const int32_t* first, int32_t* table, int32_t table_width, int32_t* cu, int32_t* lens,
                                    int64_t* slots, int32_t max_add, int32_t* first_out, void* stream) {
-  if (!held || !add || !free_pages || !first || !table || !cu || !lens || !first_out || (!slots && max_add > 0)) return FASTAR_ERR_INVALID_ARG;
+  if (!held || !add || (!free_pages && num_free != 0) || !first || !table || !cu || !lens || !first_out || (!slots && max_add > 0)) return FASTAR_ERR_INVALID_ARG;
   if (num_seqs < 1 || num_free < 0 || table_width < 1 || max_add < 0 || first == first_out || held == lens || add == lens) return FASTAR_ERR_INVALID_ARG;
   if ((page_tokens != 64 && page_tokens != 128) || num_seqs > kMostSeqs || max_add > kMostRows) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (!aligned(held, 4) || !aligned(add, 4) || !aligned(free_pages, 4) || !aligned(first, 4) || !aligned(table, 4) || !aligned(cu, 4) || !aligned(lens, 4) ||

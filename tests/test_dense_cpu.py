@@ -98,6 +98,20 @@ def test_table_limits(lib, mem, bad):
     assert lib.fastar_block_tables(*table_args(mem[0], cu=mem[0] + 192, **bad)) == -2
 
 
+def test_empty_free_list_is_no_bad_argument(lib, mem):
+    """A list without pages may be a null pointer (an empty tensor's is): requests that need no page are served without it.  (What follows the checks here is that
+    there is no GPU.)"""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would run with host pointers")
+    p = mem[0]
+    args = dict(cu=p + 192, free=None, num_free=0)
+    assert lib.fastar_block_tables(*table_args(p, **args)) not in (-1, -2)
+    assert lib.fastar_block_tables(*table_args(p, **args, max_add=-1)) == -1
+    assert lib.fastar_block_tables(*table_args(p, **args, seqs=0)) == -1
+    assert lib.fastar_block_tables(*table_args(p, **dict(args, num_free=1))) == -1
+
+
 def test_arguments_as_words(lib, mem):
     """fastar_dense_call takes the calls' arguments as 64-bit words and answers as they do; a count or a 32-bit argument that is not theirs is refused."""
     from paper_2602_01801_b200 import fastar

@@ -139,3 +139,19 @@ def test_outputs_straight_into_the_sparse_step(fastar, search_bits, probe):  # n
             assert x.keys() == y.keys()
             for name in x:
                 assert torch.equal(x[name], y[name]), name
+
+
+# ------------------------------------------------------------------------------------- tables
+def test_tables_without_free_pages(fastar):  # noqa: F811
+    """The free list is used up: who needs no page is served, who needs one is refused, and nothing else changes."""
+    none = torch.empty(0, dtype=torch.int32, device=base.DEV)
+    t = base.i32([[4, 2], [7, -1]])
+    got = fastar.block_tables(base.i32([70, 10]), base.i32([3, 54]), 64, none, base.i32([0]), t, 57)
+    assert got["lens"].tolist() == [73, 64] and got["cu"].tolist() == [0, 3, 57] and got["first"].tolist() == [0]
+    assert got["slots"].tolist() == [2 * 64 + 6 + i for i in range(3)] + [7 * 64 + 10 + i for i in range(54)]
+    assert fastar.dense_last_status() == 0
+    got = fastar.block_tables(base.i32([70, 10]), base.i32([3, 55]), 64, none, base.i32([0]), t, 58)
+    assert got["lens"].tolist() == [73, -1] and got["cu"].tolist() == [0, 3, 58] and got["first"].tolist() == [0]
+    assert got["slots"].tolist() == [2 * 64 + 6 + i for i in range(3)] + [-1] * 55
+    assert t.tolist() == [[4, 2], [7, -1]]
+    assert fastar.dense_last_status() == fastar.ERR_CAPACITY
