@@ -403,9 +403,10 @@ int fastar_noalloc_last_status(void* stream);
  * it need (requests whose row is too short need nothing); one that needs no page is never refused for the list.  Outputs: table (new
  * entries of accepted requests written, all others left), cu [num_seqs + 1] (prefix sums of add, refused requests included), lens
  * [num_seqs] (held + add, or -1), slots [max_add] int64 (page * page_tokens + row of every new token; -1 for refused ones and from the
- * last token on), first_out [1] (first + pages taken).  held, add, first: dev int32; first_out and lens are not in place.  Tokens beyond
- * max_add are cut off and their requests refused, negative lengths refuse the request (FASTAR_ERR_BOUNDS in the status word); a list
- * that is too short leaves FASTAR_ERR_CAPACITY there.  An empty list may be null. */
+ * last token on), first_out [1] (first + pages taken).  held, add, first: dev int32; what is written lies apart from what is read
+ * (inputs may overlap one another).  Tokens beyond max_add are cut off and their requests refused, negative lengths refuse the
+ * request (FASTAR_ERR_BOUNDS in the status word); a list that is too short leaves FASTAR_ERR_CAPACITY there.  An empty list may be
+ * null. */
 int fastar_block_tables(const int32_t* held, const int32_t* add, int32_t num_seqs, int32_t page_tokens, const int32_t* free_pages,
                         int32_t num_free, const int32_t* first, int32_t* table, int32_t table_width, int32_t* cu, int32_t* lens,
                         int64_t* slots, int32_t max_add, int32_t* first_out, void* stream);

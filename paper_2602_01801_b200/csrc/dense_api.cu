@@ -44,6 +44,14 @@ int dense_device(int32_t** status) {
 }
 
 bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+struct Span {                      // bytes of an array
+  const void* p;
+  int64_t bytes;
+};
+bool apart(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x <= y ? y - x >= static_cast<uint64_t>(a.bytes) : x - y >= static_cast<uint64_t>(b.bytes);
+}
 // Rows of `heads` heads: 16-byte pieces, not overlapping (a stride over one head or one token is not used)
 bool rows_ok(const void* p, int64_t hs, int64_t ts, int heads, int tokens, int d) {
   return p && aligned(p, 16) && (tokens == 1 || (ts >= d && ts % 8 == 0)) && (heads == 1 || (hs >= d && hs % 8 == 0));
@@ -146,11 +154,22 @@ extern "C" int fastar_block_tables(const int32_t* held, const int32_t* add, int3
                                    int32_t num_free, const int32_t* first, int32_t* table, int32_t table_width, int32_t* cu, int32_t* lens,
                                    int64_t* slots, int32_t max_add, int32_t* first_out, void* stream) {
   if (!held || !add || (!free_pages && num_free != 0) || !first || !table || !cu || !lens || !first_out || (!slots && max_add > 0)) return FASTAR_ERR_INVALID_ARG;
-  if (num_seqs < 1 || num_free < 0 || table_width < 1 || max_add < 0 || first == first_out || held == lens || add == lens) return FASTAR_ERR_INVALID_ARG;
+  if (num_seqs < 1 || num_free < 0 || table_width < 1 || max_add < 0) return FASTAR_ERR_INVALID_ARG;
   if ((page_tokens != 64 && page_tokens != 128) || num_seqs > kMostSeqs || max_add > kMostRows) return FASTAR_ERR_UNSUPPORTED_SHAPE;
   if (!aligned(held, 4) || !aligned(add, 4) || !aligned(free_pages, 4) || !aligned(first, 4) || !aligned(table, 4) || !aligned(cu, 4) || !aligned(lens, 4) ||
       !aligned(slots, 8) || !aligned(first_out, 4))
     return FASTAR_ERR_INVALID_ARG;
+  // every CTA reads all requests, and one writes the outputs
+  const int64_t n = num_seqs;
+  const Span out[5] = {{table, 4 * n * table_width}, {cu, 4 * (n + 1)}, {lens, 4 * n}, {first_out, 4}, {slots, 8 * static_cast<int64_t>(max_add)}};
+  const Span in[4] = {{held, 4 * n}, {add, 4 * n}, {free_pages, 4 * static_cast<int64_t>(num_free)}, {first, 4}};
+  for (int o = 0; o < 5; ++o) {
+    if (out[o].bytes == 0) continue;
+    for (const Span& x : in)
+      if (x.bytes > 0 && !apart(out[o], x)) return FASTAR_ERR_INVALID_ARG;
+    for (int x = 0; x < o; ++x)
+      if (!apart(out[o], out[x])) return FASTAR_ERR_INVALID_ARG;
+  }
   int32_t* status = nullptr;
   const int r = dense_device(&status);
   if (r != FASTAR_OK) return r;

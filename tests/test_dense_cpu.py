@@ -98,6 +98,23 @@ def test_table_limits(lib, mem, bad):
     assert lib.fastar_block_tables(*table_args(mem[0], cu=mem[0] + 192, **bad)) == -2
 
 
+def test_tables_are_not_in_place(lib, mem):
+    """Every CTA of the tables' kernel reads all requests by itself, so what one writes must lie apart from what the others read, and outputs apart from one another."""
+    p = mem[0]
+    at = dict(held=p, add=p + 64, free=p + 128, first=p + 192, table=p + 256, cu=p + 320, lens=p + 384, slots=p + 512, first_out=p + 640)
+    size = dict(held=8, add=8, free=12, first=4, table=32, cu=12, lens=8, slots=64, first_out=4)
+    outputs = ("table", "cu", "lens", "slots", "first_out")
+    import torch
+    if not torch.cuda.is_available():                                          # (there it would run with host pointers)
+        assert lib.fastar_block_tables(*table_args(p, **at)) not in (-1, -2)
+        assert lib.fastar_block_tables(*table_args(p, **dict(at, held=p, add=p, lens=p + 8, cu=p + 16, first_out=p + 28))) not in (-1, -2)      # side by side, one input twice
+    for out in outputs:
+        for other in at:
+            if other != out:
+                for place in (at[other], at[other] + (size[other] - 1) // 8 * 8, at[other] - (size[out] - 1) // 8 * 8):
+                    assert lib.fastar_block_tables(*table_args(p, **dict(at, **{out: place}))) == -1, (out, other, place - at[other])
+
+
 def test_empty_free_list_is_no_bad_argument(lib, mem):
     """A list without pages may be a null pointer (an empty tensor's is): requests that need no page are served without it.  (What follows the checks here is that
     there is no GPU.)"""
@@ -105,7 +122,7 @@ def test_empty_free_list_is_no_bad_argument(lib, mem):
     if torch.cuda.is_available():
         pytest.skip("would run with host pointers")
     p = mem[0]
-    args = dict(cu=p + 192, free=None, num_free=0)
+    args = dict(add=p + 64, first=p + 128, table=p + 256, cu=p + 320, lens=p + 384, slots=p + 512, first_out=p + 640, free=None, num_free=0)
     assert lib.fastar_block_tables(*table_args(p, **args)) not in (-1, -2)
     assert lib.fastar_block_tables(*table_args(p, **args, max_add=-1)) == -1
     assert lib.fastar_block_tables(*table_args(p, **args, seqs=0)) == -1
