@@ -6,7 +6,7 @@
 // a ring and a soft-max of its own, so that nobody waits for anybody until the end of a piece, where the four are added up in shared memory.
 //   - Keys are the products' rows (m16n8k16: 16 keys x 8 query rows), so one token's few rows fill an instruction, and 8, 16 or 32 rows share a key's conversion.
 //   - fp16 operands: e4m3 values are fp16 values, and one instruction converts two.  Queries are divided by a power of two so that the row's largest is in [1, 2):
-//     fp16 then holds them to 2^-25 of it, better than their own type.  Probabilities are 2^8 at most.
+//     fp16 then holds them to 2^-25 of it, better than their own type.  Probabilities are 2^15 at most (kHalfLift).
 //   - The order of the d products of a logit is free, so a thread takes 32 neighbouring codes of a key (two 16-byte reads) as its part of eight k-steps.
 //   - Values come through ldmatrix.trans as pairs of neighbouring columns; even and odd columns are rows 0-7 and 8-15 of the product's first operand, so one byte
 //     permutation makes two operands.  Probabilities turn by movmatrix.
@@ -23,7 +23,7 @@
 namespace fastar {
 
 constexpr int kFewThreads = 128;
-constexpr float kFewRaise = 8.f;                                   // the reference is raised when a logit exceeds it by so many binary orders
+constexpr float kFewRaise = kHalfLift + 8.f;                       // the reference is raised when a logit exceeds it by so many binary orders, to kHalfLift below it
 constexpr float kLeastScale = 1.17549435e-38f, kUnitSpan = 8.67361738e-19f;      // 2^-126, 2^-60
 
 // NR: groups of 8 rows; TILE keys of a warp's tile, in STAGES stages
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) mx[n][h] = fmaxf(mx[n][h], __shfl_xor_sync(0xffffffffu, mx[n][h], w));
-            const float top = fmaxf(m[n][h], mx[n][h]);
+            const float top = fmaxf(m[n][h], mx[n][h] - kHalfLift);
             alpha[h] = m[n][h] == -INFINITY ? 0.f : fast_exp2(m[n][h] - top);
             m[n][h] = top;
           }

@@ -7,8 +7,9 @@
 //   O_t += P_t V_j                tcgen05.mma, TMEM x shared memory
 // TMEM holds two S of 128 columns and two O of d.  At d = 128 that is all of it: P takes the place of its S, and a tile goes in two halves of 64 keys, so that the
 // products of one half run while the other is in its exponentials.  At d = 64 P lies beside, and Q K^T of the next tile follows as soon as the logits are in registers.
-// The running maximum is raised only when a logit exceeds it by 8 binary orders (O is rescaled then, by the warps that own its rows); sums add up the
-// probabilities as rounded.  Some of the exponentials go to the FMA units.
+// The reference of the exponentials is raised only when a logit exceeds the maximum it was taken from by 8 binary orders (O is rescaled then, by the warps that own its
+// rows); it is that maximum where probabilities are bf16, and kHalfLift below it where they are fp16.  Sums add up the probabilities as rounded.  Some of the
+// exponentials go to the FMA units.
 // 8-bit cache: four warps read codes, two tiles ahead in registers, convert them to fp16 (exact) and put them where TMA would have put them.  Queries are fp16
 // too, their row divided by a power of two; a page's key scale goes into the factor of the logits, value scales are taken relative to the largest of the
 // CTA's keys (a power of two, so nothing is rounded within 2^15 of it, and a value by 2^-14 of its page's largest at most within 2^18; beyond that, and where there are NaN
@@ -84,6 +85,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   using SM = ManySmem<D>;
   using M = typename std::conditional<PAGED, __half, T>::type;     // the products' type
   constexpr bool kHalf = std::is_same<M, __half>::value;
+  constexpr float kLift = kHalf ? kHalfLift : 0.f;
   constexpr bool kOver = D == 128;                                 // P lies over S: there is no more room in tensor memory
   constexpr int kSub = ManyRoles<D>::kSub, NS = kKeys / kSub;      // parts of a key tile
   constexpr int SK = SM::SK, SV = SM::SV;
@@ -593,9 +595,9 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
         if (!ok) break;
         tc_fence_after();
       }
-      const bool raise = !(top <= m + kRaise);                     // (at first m is -inf; a logit that is no number makes m, and with it all, none)
+      const bool raise = !(top <= m + (kRaise + kLift));           // (at first m is -inf; a logit that is no number makes m, and with it all, none)
       if (__any_sync(0xffffffffu, raise)) {
-        const float to = raise ? top : m, alpha = to == m ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - to);
+        const float to = raise ? top - kLift : m, alpha = to == m ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - to);
         m = to;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {

@@ -37,6 +37,11 @@ __device__ __forceinline__ void add_f16x2(float2& s, uint32_t b) {
   asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.f16 %0, l, %0; add.f32.f16 %1, h, %1;}" : "+f"(s.x), "+f"(s.y) : "r"(b));
 }
 
+// fp16 probabilities are taken relative to a reference that lies so many binary orders below the largest logit it was taken from.  The reference is raised when a logit
+// exceeds it by kHalfLift + 8, so they are 2^15 at most, and those of keys down to 2^-21 of the row's largest at least (2^-29 at best) keep all their bits: relative to the
+// largest itself it would be 2^-14, and thousands of keys at 2^-20 beside one that has no value of its own were off by up to 3 %.
+constexpr float kHalfLift = 7.f;
+
 // What a logit is multiplied by: the power of two that its query row was divided by, 1 / sqrt(d), and the scale of its key's page.  The product of queries below 2^-20 and
 // a page of zero keys (scale 2^-126) would round to 0, and that of large ones overflow: kept positive and finite, -inf stays what it is where a key is not seen, and a
 // logit of 0 too.  Logits that the lower end scales are below 2^-100 either way.

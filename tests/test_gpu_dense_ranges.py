@@ -155,3 +155,53 @@ def test_tables_without_free_pages(fastar):  # noqa: F811
     assert got["slots"].tolist() == [2 * 64 + 6 + i for i in range(3)] + [-1] * 55
     assert t.tolist() == [[4, 2], [7, -1]]
     assert fastar.dense_last_status() == fastar.ERR_CAPACITY
+
+
+# ------------------------------------------------------------------------------------- many small weights beside a large one
+# One key has a logit some 19.5 to 20.5 binary orders above all others' and a value of zero, so that an output is the sum of thousands of weights of 2^-20.
+# A weight may be off by half a step of its type, not more, for the sum to stay within what the test's bound gives it.
+ABOVE = 20.5
+
+
+def sink_queries(g, H, T, D, dt):
+    c = ABOVE / (D ** 0.5 * 1.4426950408889634)                # every column of q; the key's are 1
+    return ((0.951 + 0.048 * torch.rand(H, T, 1, generator=g, device=base.DEV)) * c).to(dt).expand(H, T, D).contiguous()
+
+
+@pytest.mark.parametrize("B,n,past,H,KV", [(100, 1, 2000, 8, 8), (60, 4, 2000, 8, 8), (1, 140, 4000, 2, 2)])
+@pytest.mark.parametrize("dtype,D", [("fp16", 64), ("bf16", 128), ("fp16", 128)])
+def test_paged_small_weights_add_up(fastar, B, n, past, H, KV, dtype, D):  # noqa: F811
+    g, dt, PT = base.gen(51), base.TYPES[dtype], 64
+    L = past + n
+    W = -(-L // PT)
+    pool = base.Pool(B * W, KV, PT, D)
+    table = torch.randperm(B * W, generator=g, device=base.DEV).to(torch.int32).view(B, W)
+    pool.codes[0].zero_()
+    pool.codes[1].copy_(torch.randint(0x30, 0x40, pool.codes[1].shape, generator=g, device=base.DEV, dtype=torch.uint8))       # 0.5 to 1.875
+    pool.scale[0].fill_(1.0)
+    pool.scale[1].fill_(1.0)
+    pool.codes[0][table[:, 0].long(), :, 0] = 0x38                             # 1.0
+    pool.codes[1][table[:, 0].long(), :, 0] = 0
+    q = sink_queries(g, H, B * n, D, dt)
+    cu, lens = base.prefix([n] * B), [L] * B
+    out = fastar.kv8_attention(q, *pool.args(), table, base.i32(lens), base.i32(cu), n, L)
+    G = H // KV
+    o, bound = base.R.attention(q, lambda b, h: pool.rows(0, table[b], L, h // G), lambda b, h: pool.rows(1, table[b], L, h // G), cu, lens, 1, dt)
+    base.check(out, o, bound, cu)
+
+
+@pytest.mark.parametrize("dtype,D", [("fp16", 64), ("fp16", 128), ("bf16", 128)])
+def test_packed_small_weights_add_up(fastar, dtype, D):  # noqa: F811
+    """(A row that sees few keys has an output below 2^-14, whose fp16 numbers are 2^-24 apart, so that rounding it is off by up to 2^-25 and not by u |o| only.)"""
+    dt = base.TYPES[dtype]
+    for H, KV, n, frame in ((2, 2, 3000, 0), (4, 2, 1500, 1)):
+        g = base.gen(1)
+        q, k, v = (base.rows(g, heads, n, D, dt) for heads in (H, KV, KV))
+        q.copy_(sink_queries(base.gen(52), H, n, D, dt))
+        k.zero_()
+        k[:, 0] = 1.0
+        v.copy_(v.abs() + 0.5)
+        v[:, 0] = 0.0
+        out = fastar.packed_attention(q, k, v, base.i32([0, n]), n, frame_len=frame)
+        o, bound = base.R.attention(q, lambda b, h: k[h // (H // KV)].double(), lambda b, h: v[h // (H // KV)].double(), [0, n], [n], frame, dt)
+        base.check(out, o, bound + (2.0 ** -25 if dtype == "fp16" else 0.0), [0, n])
