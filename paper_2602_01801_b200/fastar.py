@@ -465,11 +465,16 @@ def _int_ok(i32, dev, t) -> bool:
     return t.dtype == i32 and t.get_device() == dev and t.is_contiguous()
 
 
+def _strides_fit(shape, a, b) -> bool:
+    """The same places: a stride over one head or token is not used, nor is any where there is none."""
+    return a == b or shape[1] == 0 or (a[2] == b[2] and (a[0] == b[0] or shape[0] == 1) and (a[1] == b[1] or shape[1] == 1))
+
+
 def _out_like(torch, q, strides, out, where):
     if out is None:
         out = torch.empty_like(q)
         return out if out.stride() == strides else torch.empty_strided(q.shape, strides, dtype=q.dtype, device=q.device)
-    if out.dtype != q.dtype or out.get_device() != q.get_device() or out.shape != q.shape or out.stride() != strides:
+    if out.dtype != q.dtype or out.get_device() != q.get_device() or out.shape != q.shape or not _strides_fit(q.shape, out.stride(), strides):
         _refuse(where)
     return out
 
@@ -500,7 +505,7 @@ def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu
     lib, torch, dtypes, i32, _, _, current = _dense or _dense_init()
     where, dev = "kv8_append", k_new.get_device()
     dtype, shape, strides = dtypes.get(k_new.dtype), k_new.shape, k_new.stride()
-    if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and v_new.dtype == k_new.dtype and v_new.shape == shape and v_new.stride() == strides
+    if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and v_new.dtype == k_new.dtype and v_new.shape == shape and _strides_fit(shape, v_new.stride(), strides)
             and v_new.get_device() == dev and k_codes.dim() == 4 and _pools_ok(torch, dev, k_codes, v_codes, k_scale, v_scale)):
         _refuse(where)
     (P, KV, PT, D), B = k_codes.shape, lens.shape[0]
@@ -548,7 +553,7 @@ def packed_attention(q, k, v, cu, max_tokens: int, frame_len: int = 1, out=None)
     where, dev = "packed_attention", q.get_device()
     dtype, shape, strides, kv_shape, kv_strides = dtypes.get(q.dtype), q.shape, q.stride(), k.shape, k.stride()
     if not (dev >= 0 and dtype is not None and len(shape) == 3 and strides[2] == 1 and len(kv_shape) == 3 and kv_strides[2] == 1 and k.dtype == q.dtype and v.dtype == q.dtype
-            and v.shape == kv_shape and v.stride() == kv_strides and k.get_device() == dev and v.get_device() == dev and kv_shape[1:] == shape[1:]
+            and v.shape == kv_shape and _strides_fit(kv_shape, v.stride(), kv_strides) and k.get_device() == dev and v.get_device() == dev and kv_shape[1:] == shape[1:]
             and cu.dim() == 1 and cu.shape[0] >= 2 and _int_ok(i32, dev, cu)):
         _refuse(where)
     if dev != current():

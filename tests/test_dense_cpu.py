@@ -181,3 +181,22 @@ def test_index_arithmetic(tmp_path):
     assert r.returncode == 0, r.stderr
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "ok" in r.stdout, r.stdout + r.stderr
+
+
+def test_strides_over_one_head_or_token_do_not_count():
+    """Outputs (and values beside keys) whose strides differ only where there is one head, one token or none are taken, others refused."""
+    import torch
+    from paper_2602_01801_b200 import fastar
+    wide = torch.zeros(4, 3, 5, 64, dtype=torch.bfloat16)                      # queries, keys and values of five tokens in one tensor, by heads
+    rows = torch.zeros(5, 12, 64, dtype=torch.bfloat16).transpose(0, 1)        # and by tokens
+    for q in (rows[:4, :1], wide[:1, 1], wide[:1, 2, :1], rows[8:9, 4:], wide[:, 0, :0]):
+        out = torch.zeros(q.shape, dtype=q.dtype)
+        assert fastar._out_like(torch, q, q.stride(), out, "here") is out
+        made = fastar._out_like(torch, q, q.stride(), None, "here")
+        assert made.shape == q.shape and fastar._strides_fit(q.shape, made.stride(), q.stride())
+    for q in (wide[:, 0, :2], wide[:, 0, :1], rows[:1]):
+        with pytest.raises(fastar.FastarError):
+            fastar._out_like(torch, q, q.stride(), torch.zeros(q.shape, dtype=q.dtype), "here")
+    with pytest.raises(fastar.FastarError):
+        fastar._out_like(torch, wide[:1, 0], wide[:1, 0].stride(), torch.zeros(1, 5, 128, dtype=q.dtype)[..., ::2], "here")      # columns apart
+    assert fastar._strides_fit((4, 1, 64), (960, 7, 1), (960, 64, 1)) and not fastar._strides_fit((4, 2, 64), (960, 7, 1), (960, 64, 1))

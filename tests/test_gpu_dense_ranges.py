@@ -205,3 +205,26 @@ def test_packed_small_weights_add_up(fastar, dtype, D):  # noqa: F811
         out = fastar.packed_attention(q, k, v, base.i32([0, n]), n, frame_len=frame)
         o, bound = base.R.attention(q, lambda b, h: k[h // (H // KV)].double(), lambda b, h: v[h // (H // KV)].double(), [0, n], [n], frame, dt)
         base.check(out, o, bound + (2.0 ** -25 if dtype == "fp16" else 0.0), [0, n])
+
+
+# ------------------------------------------------------------------------------------- strides
+@pytest.mark.parametrize("H,KV", [(4, 4), (4, 1), (1, 1)])
+def test_one_token_out_of_wider_rows(fastar, H, KV):  # noqa: F811
+    """A single token's queries, keys and values as views of one projection's output, into a contiguous output."""
+    g, D, dt = base.gen(61), 64, torch.bfloat16
+    wide = base.rows(g, 1, 1, (H + 2 * KV) * D, dt).view(1, H + 2 * KV, D).transpose(0, 1)     # [heads][1][D]
+    q, k, v = wide[:H], wide[H: H + KV], wide[H + KV:].contiguous()
+    out = torch.zeros(H, 1, D, dtype=dt, device=base.DEV)
+    got = fastar.packed_attention(q, k, v, base.i32([0, 1]), 1, out=out)
+    assert got is out and torch.equal(out, v.repeat_interleave(H // KV, 0))
+    pool = base.Pool(1, KV, 64, D)
+    table, lens, cu = base.i32([[0]]), base.i32([1]), base.i32([0, 1])
+    fastar.kv8_append(k, v, *pool.args(), table, lens, cu)
+    want = fastar.kv8_attention(q.contiguous(), *pool.args(), table, lens, cu, 1, 1)
+    assert torch.equal(fastar.kv8_attention(q, *pool.args(), table, lens, cu, 1, 1, out=out), want)
+    assert torch.equal(want.double(), pool_values(pool)[0, :, :1].repeat_interleave(H // KV, 0))
+
+
+def pool_values(pool):
+    """[pages][heads][rows][D] of the values, in 64 bits (exact in bf16)."""
+    return base.R.e4m3_values(base.DEV)[pool.codes[1].long()] * pool.scale[1].double()[:, :, None, None]
