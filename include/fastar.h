@@ -390,12 +390,15 @@ int fastar_noalloc_last_status(void* stream);
  * Frames: a token sees the keys of its sequence up to the end of its own frame of frame_len tokens (positions
  * [0, (floor(position / frame_len) + 1) frame_len)), frame_len = 1 being the causal mask; 0: all keys of the sequence.
  * What is not seen has no influence, whatever its bits are.  A row that sees only logits of -inf gives zeros.
- * max_new, max_len: what no n_b and no lens[b] exceeds (they size the launch; 1 <= max_new, max_new <= max_len).
+ * max_new, max_len: what no n_b and no lens[b] exceeds; 1 <= max_new <= max_len, and max_len <= table_width x page_tokens.  They size the
+ * launch: chunks of many rows are cut into parts by max_len, so that one far above the lengths leaves them in fewer parts, on fewer SMs
+ * (single tokens and a few rows are cut by the lengths themselves).
  * The device used is the current one.  Lengths, tables and page numbers that the host cannot see are checked on the
- * device: a sequence whose entries are out of range (cu not ascending within [0, T], n_b > max_new, lens[b] > max_len, lens[b] <
- * n_b) is passed over, a page outside the pool is not written and page 0 is read in its place; the first such finding stays in
- * a status word of the library (FASTAR_ERR_BOUNDS) until fastar_dense_last_status reads it.  The first of these calls on a
- * device looks that word up; make it before any stream capture starts.  Later calls may be captured. */
+ * device: a sequence whose entries are out of range (cu[b], cu[b + 1] not ascending within [0, T], n_b > max_new, lens[b] > max_len,
+ * lens[b] < n_b) is passed over, a page outside the pool is not written and page 0 is read in its place; the first such finding stays in
+ * a status word of the library (FASTAR_ERR_BOUNDS) until fastar_dense_last_status reads it.  Where cu falls and rises again, so that two
+ * sequences have the same tokens, what these rows get is not defined.  The first of these calls on a device looks the status word up;
+ * make it before any stream capture starts.  Later calls may be captured. */
 
 /* Page tables and slots from the requests' lengths.  Request b holds held[b] tokens in the first ceil(held[b] / page_tokens) pages
  * of its row and adds add[b]; the pages that this takes come off the free list free_pages[first .. num_free), in the order of the
@@ -424,7 +427,12 @@ int fastar_kv8_append(const void* k_new, const void* v_new, int64_t head_stride,
 /* Attention of the new tokens (q, out: dev [num_heads][T][d], same strides) over the cache, their own keys included (append first).
  * One token a sequence, a few, or thousands; sequences of all lengths in one call.  workspace: dev, 16-byte aligned, of at least
  * fastar_kv8_attention_workspace_bytes (0 on invalid arguments; else 16 or more; with 16 none is used, and it may be null), contents
- * irrelevant before and after; it belongs to one call at a time. */
+ * irrelevant before and after; it belongs to one call at a time.
+ * How far the value scales of a sequence's pages may lie apart: for up to 32 rows (tokens x query heads of a key head) a sequence, values of a page
+ * whose scale is below 2^-60 of the largest among the keys before it lose bits, and all of them below 2^-92.  Above 32 rows, those of a page with the
+ * least scale of all, 2^-126, do so beside a scale of more than 2^-108; any other page below 2^-18 of its key head's largest, like a NaN code in a
+ * page that some row does not see as a whole, has its CTAs' 256 rows worked out key by key, which is right but slow: 1 560 queries over 29 640
+ * keys, 12 heads, take 64 ms with one such page and 0.39 without, 140 over 4 096 take 4.1 and 0.05. */
 size_t fastar_kv8_attention_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t max_new, int32_t max_len, int32_t num_heads,
                                             int32_t num_kv_heads, int32_t head_dim);
 int fastar_kv8_attention(const void* q, void* out, int64_t head_stride, int64_t token_stride, const uint8_t* k_codes, const uint8_t* v_codes,

@@ -89,6 +89,10 @@ struct AttendPlan {
   int chunk, parts;
   size_t few_o, few_ml, few_pieces, part_o, part_ml, bytes;        // offsets
 };
+// Up to so many rows (tokens x query heads of a key head) a sequence has the kernel for few rows; it reads and converts every code once for 16 of them at d = 128, for 32 at
+// 64, the one for many once for 256.  32 sequences of 8 192 keys, 12 heads, d = 128, us there / here: 20 rows 256 / 477, 32 rows 267 / 447, 33-48 rows 403 / 469,
+// 64 rows 546 / 457, 96 rows 823 / 439; d = 64: 32 rows 148 / 345, 64 rows 274 / 356, 96 rows 397 / 346.  One sequence of 32 768 keys, d = 128: 24 rows 44 / 60, 40 rows 59 / 60,
+// 64 rows 74 / 62.  (Floors by bytes: 122 and 61 us for the 32 sequences, 15 for the one.)
 constexpr int kFewRows = 32;
 constexpr int kSms = 148;
 AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, int D) {
@@ -106,7 +110,8 @@ AttendPlan attend_plan(int B, int T, int max_new, int max_len, int H, int KV, in
     const int64_t items = static_cast<int64_t>(B) * KV * p.few_row_tiles, units = items * tiles, most = few_ctas_an_sm(p.few_tile, D) * kSms;
     p.few_ctas = static_cast<int>(units < most ? units : most);
     p.join = tiles > 1;
-    // A cluster an item, where none has more than four tiles a CTA and all are on the SMs at once
+    // A cluster an item, where none has more than four tiles a CTA and all are on the SMs at once.  One token, us with clusters / cut items: 4 096 keys (four tiles a CTA),
+    // one sequence of 12 heads 12.6 / 10.9, four 17.4 / 17.9; 8 192 keys 18.8 / 14.8 and 27.6 / 26.8.  Up to 2 048 keys cut items have the join's launch on top of 7.6-12.5.
     int share = 8;
     while (share > 1 && share > tiles) share /= 2;
     if (items * share <= most && tiles <= 4 * share) {

@@ -13,8 +13,8 @@
 //   - A page's value scale is a unit of the accumulators: they are multiplied by a power of two where it changes from page to page, exactly.  The unit is kept
 //     within 2^60 of the largest seen, so that a page of zeros (scale 2^-126) does not take the sums out of range.
 //   - The row sums add up the probabilities as rounded.
-// Measured (B200, us): one token each of eight sequences of 65 536 keys, 40 query and 8 key heads 172 (6.2 TB/s of codes, 187 at the power limit), with rows as the products'
-// first operand, 16 of them, and a CTA for every 4 096 keys 282; of 32 sequences of 1 to 16 384 keys 65 (4.9 TB/s) after 134; of 512 sequences of up to 1 000 keys 89-102.
+// Measured (B200, us): one token each of eight sequences of 65 536 keys, 40 query and 8 key heads 174-191 (6.2 TB/s of codes cool, 5.6 at the power limit), with rows as the products'
+// first operand, 16 of them, and a CTA for every 4 096 keys 282; of 32 sequences of 1 to 16 384 keys 66-68 (4.8 TB/s) after 134; of 512 sequences of up to 1 000 keys 89-102.
 // Two CTAs an SM with tiles of 32 keys: 67, 121 for the last two.
 #include "common.h"
 #include "dense.h"
@@ -687,7 +687,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
 }
 
 // Rows of an item where a sequence has so many at most.  32 rows of 128 columns do not fit the registers; two items of 16 read the keys twice, the second time
-// out of L2 (32 sequences of 24 tokens, 12 heads, 8 192 keys on average: 544 us as one item, with 700 bytes a thread spilled, 404 as two).
+// out of L2 (32 sequences of 24 tokens, 12 heads, 8 192 keys on average: 544 us as one item, with 700 bytes a thread spilled, 404 as two; of 8 192 keys each 262).
+// 32 rows of 64 columns fit but for some 100 bytes a thread, and take 143 us there, 16 rows 102.
 int few_tile_of(int64_t rows, int D) { return rows <= 8 ? 8 : rows <= 16 || D == 128 ? 16 : 32; }
 
 template <class T, int D>

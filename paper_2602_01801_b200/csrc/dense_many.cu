@@ -16,12 +16,13 @@
 // codes in a tile that some row does not see as a whole, the rows are worked out from the definition).
 // What a row does not see must not reach it: V rows behind the last visible key are zeroed, and values that are not finite in a tile that some row does not see as
 // a whole are taken out, and all rows of the CTA are worked out from the definition afterwards (dense_rows.cuh).
-// What bounds it: at d = 128 the card's power limit (990 W, 1.7 GHz of 1.965): tensor pipe 0.51 of the cycles packed, 0.40 with codes; exponentials 0.42 and 0.36.  At
-// d = 64 the soft-max warps' chain of load, maximum, exponentials, store.
-// Measured (B200, us): 16 384 tokens, 8 query and 2 key heads 515-530 (1.05 PFLOP/s); one warp issuing for both tiles, whole tiles of 128, 520-540; the same at d = 64
-// 369, whole tiles with P over S 445.  Three times 4 680 tokens, 12 heads, by frames 292-317, at d = 64 231.  1 560 queries over 29 640 8-bit keys, 12 heads 369-375: with the codes
-// one tile ahead and NaN and scale work in every tile 614, whole tiles 455, queries by one warpgroup row by row and outputs by thread 396.  What an item costs beside its
-// tiles: some 5 000 cycles, 14 500 with queries and outputs that way (25 000 over codes).
+// What bounds it: at d = 128 the card's power limit (990 W, 1.7 GHz of 1.965) with the tensor pipe 0.51 of the cycles packed and exponentials 0.42; over codes their conversion
+// (5 000 cycles a tile for 3 525 packed; tensor pipe 0.40, exponentials 0.36); where items have few tiles their start and end.  At d = 64 the soft-max warps' chain of load,
+// maximum, exponentials, store.
+// Measured (B200, us): 16 384 tokens, 8 query and 2 key heads 472 cool, 515-547 at the limit (1.03 PFLOP/s); one warp issuing for both tiles, whole tiles of 128, 520-540; the same at
+// d = 64 369, whole tiles with P over S 445.  Three times 4 680 tokens, 12 heads, by frames 292-327, at d = 64 231.  1 560 queries over 29 640 8-bit keys, 12 heads 364-380, at d = 64 287:
+// with the codes one tile ahead and NaN and scale work in every tile 614, whole tiles 455, queries by one warpgroup row by row and outputs by thread 396.  What an item costs
+// beside its tiles: some 5 000 cycles, 14 500 with queries and outputs that way (25 000 over codes).  The way from the definition (below): 64 ms for the 1 560 queries.
 // Warp roles: 0-3 and 4-7 soft-max of the two tiles (and their queries and outputs), 8-11 the codes' way in (or the look at V), 12 and 13 MMAs of the two tiles, 14 K, 15 V (TMA).
 #include <cudaTypedefs.h>
 

@@ -352,6 +352,9 @@ template <class T, int D>
 static int launch_append_t(const AppendArgs& a, cudaStream_t st) {
   // n tokens lie in no more pages than n, nor than (n - 2) / PT + 2
   const int64_t most = static_cast<int64_t>(a.T) / a.PT + 2 * static_cast<int64_t>(a.B), items = most < a.T ? most : a.T;
+  // A warp a head and tensor up to eight tokens a sequence.  us as warps / as CTAs (in replayed graphs, d = 128): 32 sequences of 8 heads, 1 token 3.1 / 4.3, 8 tokens 3.7 / 5.3, 16 4.9 / 5.5,
+  // 32 7.4 / 7.1; 512 sequences, 1 token 9.6 / 46.7, 8 14.9 / 80, 16 20 / 85, 64 55 / 131; 4 sequences of 12 heads, 8 3.6 / 3.0, 16 4.9 / 3.1, 64 8.0 / 3.4: beyond eight
+  // it depends on how many CTAs there are.
   const bool warp = a.T <= static_cast<int64_t>(a.B) * 8;
   const dim3 grid(static_cast<unsigned>(items), warp ? (2 * a.KV + kAppendWarps - 1) / kAppendWarps : a.KV, warp ? 1 : 2);
   return launch_chained(warp ? kv8_append_kernel<T, D, true> : kv8_append_kernel<T, D, false>, grid, warp ? 32 * kAppendWarps : kAppendThreads<D>, 0, st, a) == cudaSuccess

@@ -481,7 +481,7 @@ def _out_like(torch, q, strides, out, where):
 
 def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add: int) -> Dict[str, "object"]:
     """Page tables and slots on the GPU from the requests' lengths: held, add [B] int32, the free list free_pages[first:] and table [B][W], whose new
-    entries are written in place.  Returns cu [B+1], lens [B] (-1: refused), slots [max_add] int64 and first [1], where the free list goes on."""
+    entries are written in place; the free list may be empty.  Returns cu [B+1], lens [B] (-1: refused), slots [max_add] int64 and first [1], where the free list goes on."""
     lib, torch, _, i32, _, _, current = _dense or _dense_init()
     where, dev = "block_tables", held.get_device()
     if not (dev >= 0 and held.dim() == 1 and held.shape == add.shape and table.dim() == 2 and table.shape[0] == held.shape[0] and free_pages.dim() == 1
@@ -501,7 +501,7 @@ def block_tables(held, add, page_tokens: int, free_pages, first, table, max_add:
 
 
 def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu) -> None:
-    """Writes the packed rows k_new, v_new [KV][T][d] into the 8-bit pages: token i of sequence b to position lens[b] - n_b + i."""
+    """Writes the packed rows k_new, v_new [KV][T][d] (the same strides) into the 8-bit pages: token i of sequence b to position lens[b] - n_b + i."""
     lib, torch, dtypes, i32, _, _, current = _dense or _dense_init()
     where, dev = "kv8_append", k_new.get_device()
     dtype, shape, strides = dtypes.get(k_new.dtype), k_new.shape, k_new.stride()
@@ -521,8 +521,9 @@ def kv8_append(k_new, v_new, k_codes, v_codes, k_scale, v_scale, table, lens, cu
 
 
 def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_new: int, max_len: int, frame_len: int = 1, out=None):
-    """Attention of the packed new tokens q [H][T][d] over the 8-bit cache, which holds their own keys already; n_b <= max_new, lens[b] <= max_len.
-    frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  Returns out (rows of no sequence are left as they were)."""
+    """Attention of the packed new tokens q [H][T][d] over the 8-bit cache, which holds their own keys already; n_b <= max_new, lens[b] <= max_len, which the
+    table's width reaches.  frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  out has q's strides; without it a new tensor is made.
+    Returns out: rows of no sequence, and those of a refused one (lens[b] < 0), are left as they were, so that in a new tensor they hold anything."""
     lib, torch, dtypes, i32, u8, _, current = _dense or _dense_init()
     where, dev = "kv8_attention", q.get_device()
     dtype, shape, strides = dtypes.get(q.dtype), q.shape, q.stride()
@@ -548,7 +549,8 @@ def kv8_attention(q, k_codes, v_codes, k_scale, v_scale, table, lens, cu, max_ne
 
 def packed_attention(q, k, v, cu, max_tokens: int, frame_len: int = 1, out=None):
     """Attention of packed sequences over their own tokens: q [H][T][d], k and v [KV][T][d], H a multiple of KV; no sequence is longer than max_tokens.
-    frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  Returns out (rows of no sequence are left as they were)."""
+    frame_len: 1 causal, f > 1 causal by frames of f tokens, 0 no mask.  out has q's strides; without it a new tensor is made.  Returns out: rows of no
+    sequence are left as they were, so that in a new tensor they hold anything."""
     lib, torch, dtypes, i32, _, _, current = _dense or _dense_init()
     where, dev = "packed_attention", q.get_device()
     dtype, shape, strides, kv_shape, kv_strides = dtypes.get(q.dtype), q.shape, q.stride(), k.shape, k.stride()
