@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
       int e = static_cast<int>(most >> 23) - 127;
-      e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));      // (a row that is not finite stays as it is)
+      e = most == 0 ? 0 : e == 128 ? 113 : max(-126, min(126, e));        // (a row that is not finite: its finite numbers stay so, 2^15 at most)
       const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
       const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (rsqrtf(static_cast<float>(D)) * 1.4426950408889634f);
 #pragma unroll

@@ -525,7 +525,7 @@ many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
 #pragma unroll
             for (int w = 1; w < PPR; w <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, w));
             int e = static_cast<int>(most >> 23) - 127;
-            e = most == 0 || e == 128 ? 0 : max(-126, min(126, e));            // (a row that is not finite stays as it is)
+            e = most == 0 ? 0 : e == 128 ? 113 : max(-126, min(126, e));        // (a row that is not finite: its finite numbers stay so, 2^15 at most)
             const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * scale;
             // what the row was divided by goes to the thread that has it
             const float theirs = __shfl_sync(0xffffffffu, up, lane % RPI * PPR);

@@ -228,3 +228,36 @@ def test_one_token_out_of_wider_rows(fastar, H, KV):  # noqa: F811
 def pool_values(pool):
     """[pages][heads][rows][D] of the values, in 64 bits (exact in bf16)."""
     return base.R.e4m3_values(base.DEV)[pool.codes[1].long()] * pool.scale[1].double()[:, :, None, None]
+
+
+# ------------------------------------------------------------------------------------- logits of minus infinity over codes
+@pytest.mark.parametrize("past", [20, 6000])
+@pytest.mark.parametrize("n", [1, 5, 140])
+@pytest.mark.parametrize("dtype,big", [("bf16", 1e6), ("bf16", 3e38), ("fp16", 6e4)])
+def test_paged_logits_of_minus_infinity(fastar, n, past, dtype, big):  # noqa: F811
+    """A row with -inf against a column of positive keys sees only logits of -inf and gives zeros, whatever finite numbers stand beside it; against keys of both signs,
+    or of zero, it gives no number.  Other rows are as they were."""
+    g, dt, D, PT, KV, H = base.gen(71), base.TYPES[dtype], 128, 64, 2, 4
+    L = past + n
+    W = -(-L // PT)
+    pool, table = base.Pool(W, KV, PT, D), torch.arange(W, dtype=torch.int32, device=base.DEV).view(1, W)
+    pool.fill(g, table, [L])
+    pool.codes[0][..., 0] &= 0x7F                                              # the first column is not negative ...
+    pool.codes[0][..., 0] |= 0x08                                              # ... nor zero
+    pool.codes[0][..., 0][pool.codes[0][..., 0] == 0x7F] = 0x38
+    pool.codes[0][..., 1] = 0xB8                                               # and the second is -1
+    pool.codes[0][..., 2] = 0x38
+    pool.codes[0][:, 0, 0, 2] = 0                                              # but for one key of the first head's
+    q = base.rows(g, H, n, D, dt)
+    want = fastar.kv8_attention(q, *pool.args(), table, base.i32([L]), base.i32([0, n]), n, L)
+    spoilt = q.clone()
+    spoilt[0, -1, 0], spoilt[0, -1, 1] = -float("inf"), -big                   # -inf + a finite positive number
+    spoilt[1, 0, 2], spoilt[1, 0, 1] = float("inf"), big                       # inf x 0 where its keys have one
+    spoilt[3, 0, 0], spoilt[3, 0, 1], spoilt[3, 0, 5] = -float("inf"), -big, big
+    out = fastar.kv8_attention(spoilt, *pool.args(), table, base.i32([L]), base.i32([0, n]), n, L)
+    assert bool((out[0, -1] == 0).all()) and bool((out[3, 0] == 0).all())
+    assert bool(torch.isnan(out[1, 0]).all())
+    same = torch.ones(H, n, dtype=torch.bool, device=base.DEV)
+    same[0, -1] = same[1, 0] = same[3, 0] = False
+    assert torch.isfinite(want).all()
+    assert torch.allclose(out[same].float(), want[same].float(), rtol=2.0 ** -7, atol=2.0 ** -7)
