@@ -261,3 +261,44 @@ def test_paged_logits_of_minus_infinity(fastar, n, past, dtype, big):  # noqa: F
     same[0, -1] = same[1, 0] = same[3, 0] = False
     assert torch.isfinite(want).all()
     assert torch.allclose(out[same].float(), want[same].float(), rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
+# ------------------------------------------------------------------------------------- the first call of a kind in a capture
+def test_first_calls_in_a_capture(fastar):  # noqa: F811
+    """A process whose first call is one of the tables may capture all others without having made them before."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from tests import test_gpu_dense as base
+from paper_2602_01801_b200 import fastar
+g = base.gen(1)
+table = torch.full((2, 130), -1, dtype=torch.int32, device=base.DEV)
+free = torch.arange(260, dtype=torch.int32, device=base.DEV)
+t = fastar.block_tables(base.i32([0, 0]), base.i32([8000, 300]), 64, free, base.i32([0]), table, 8300)
+k = base.rows(g, 2, 8300, 128, torch.bfloat16)
+q = base.rows(g, 4, 8300, 128, torch.bfloat16)
+few, many = base.i32([0, 1, 3]), base.i32([0, 200, 300])
+pool = [base.Pool(260, 2, 64, 128) for _ in range(2)]
+def calls(p):
+    fastar.kv8_append(k, k, *p.args(), table, t["lens"], t["cu"])
+    fastar.kv8_append(k[:, :3], k[:, :3], *p.args(), table, t["lens"], few)
+    return [fastar.kv8_attention(q[:, :3].contiguous(), *p.args(), table, t["lens"], few, 2, 8320), fastar.kv8_attention(q[:, :300].contiguous(), *p.args(), table, t["lens"], many, 200, 8320),
+            fastar.kv8_attention(q[:, :3].contiguous(), *p.args(), table, base.i32([30, 40]) if p is pool[1] else small, few, 2, 64), fastar.packed_attention(q[:, :300].contiguous(), k[:, :300].contiguous(), k[:, :300].contiguous(), many, 200)]
+small = base.i32([30, 40])
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    got = calls(pool[0])
+graph.replay()
+want = calls(pool[1])
+torch.cuda.synchronize()
+for a, b, n in zip(got, want, (3, 300, 3, 300)):
+    assert torch.equal(a[:, :n], b[:, :n])
+assert fastar.dense_last_status() == 0
+print("equal")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "equal" in r.stdout, r.stderr[-2000:]
