@@ -396,9 +396,9 @@ int fastar_noalloc_last_status(void* stream);
  * The device used is the current one.  Lengths, tables and page numbers that the host cannot see are checked on the
  * device: a sequence whose entries are out of range (cu[b], cu[b + 1] not ascending within [0, T], n_b > max_new, lens[b] > max_len,
  * lens[b] < n_b) is passed over, a page outside the pool is not written and page 0 is read in its place; the first such finding stays in
- * a status word of the library (FASTAR_ERR_BOUNDS) until fastar_dense_last_status reads it.  Where cu falls and rises again, so that two
- * sequences have the same tokens, what these rows get is not defined.  The first of these calls on a device looks the status word up;
- * make it before any stream capture starts.  Later calls may be captured. */
+ * a status word of the library (FASTAR_ERR_BOUNDS) until fastar_dense_last_status reads it.  Where cu falls and rises again, so that
+ * sequences in range have tokens in common, what those rows get is not defined, and rows of sequences behind them may be left out.  The
+ * first of these calls on a device looks the status word up; make it before any stream capture starts.  Later calls may be captured. */
 
 /* Page tables and slots from the requests' lengths.  Request b holds held[b] tokens in the first ceil(held[b] / page_tokens) pages
  * of its row and adds add[b]; the pages that this takes come off the free list free_pages[first .. num_free), in the order of the

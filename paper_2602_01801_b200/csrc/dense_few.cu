@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
   }
 }
 
-// The sequence of token t, or -1: the last b with cu[b] <= t, by a search with 32 probes a step.
+// The sequence of token t where cu is in order: the last b with cu[b] <= t, by a search with 32 probes a step.
 __device__ __forceinline__ int seq_of_token(const DenseArgs& a, int t) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = a.B;                                             // among [lo, lo + n)
@@ -590,6 +590,25 @@ __device__ __forceinline__ int seq_of_token(const DenseArgs& a, int t) {
     lo += last * step;
   }
   return lo;
+}
+
+// Whether token t is one of a sequence that is served, and of which.  Where the search does not find it (a token of no sequence, or an entry of cu that is out of order
+// and leads it astray), all sequences are looked at.
+__device__ __forceinline__ bool owner_of_token(const DenseArgs& a, int t, int& b, DenseSeq& s) {
+  b = seq_of_token(a, t);
+  const int r = seq_of(a, b, s);
+  if (r > 0 && t >= s.t0 && t < s.t0 + s.n) return true;
+  if (r == 0 && t >= a.cu[b] && t < a.cu[b + 1]) return false;     // (refused)
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    b = b0 + (threadIdx.x & 31);
+    const uint32_t has = __ballot_sync(0xffffffffu, b < a.B && seq_of(a, b, s) > 0 && t >= s.t0 && t < s.t0 + s.n);
+    if (has) {
+      b = b0 + __ffs(has) - 1;
+      seq_of(a, b, s);
+      return true;
+    }
+  }
+  return false;
 }
 
 // Rows whose keys were cut: o = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p over the pieces p.  WARPS warps a row take its pieces in turn, four at a time, and are
@@ -604,10 +623,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const DenseArgs a) {
   const int64_t row = WARPS == 1 ? static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + warp_index() : blockIdx.x;
   if (row >= static_cast<int64_t>(a.T) * a.H) return;              // (a whole CTA, or a warp of its own)
   chain_wait();                                                    // for cu and lens too: only this makes what was written before visible here
-  const int t = static_cast<int>(row / a.H), head = static_cast<int>(row - static_cast<int64_t>(t) * a.H), b = seq_of_token(a, t);
+  const int t = static_cast<int>(row / a.H), head = static_cast<int>(row - static_cast<int64_t>(t) * a.H);
+  int b;
   DenseSeq s;
-  const int found = seq_of(a, b, s);
-  if (found <= 0 || t < s.t0 || t >= s.t0 + s.n) return;
+  if (!owner_of_token(a, t, b, s)) return;
   const bool few = s.n * a.G <= a.few_rows;
   int parts, first = 0, row_of_few = 0;
   if (few) {

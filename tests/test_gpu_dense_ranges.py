@@ -302,3 +302,34 @@ print("equal")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "equal" in r.stdout, r.stderr[-2000:]
+
+
+# ------------------------------------------------------------------------------------- prefix sums that are wrong in places
+@pytest.mark.parametrize("B,n,L", [(5, 3, 9000), (70, 3, 3000), (5, 140, 6000), (3, 700, 3000)])
+@pytest.mark.parametrize("wrong", [-1, -2 ** 31, 0, 10 ** 6, 2 ** 31 - 1])
+def test_wrong_prefix_sums_reach_their_own_sequences_only(fastar, B, n, L, wrong):  # noqa: F811
+    """One entry of cu is out of range, or below the ones before it: the two sequences that it bounds are passed over or get what the entry says (from 0 on: a range
+    that other sequences have too is not asked about), all others what they get without it, also where their keys are cut and joined."""
+    g = base.gen(81)
+    H, KV, D, PT = 4, 2, 64, 64
+    W = -(-L // PT)
+    pool, table = base.Pool(W, KV, PT, D), torch.arange(W, dtype=torch.int32, device=base.DEV).view(1, W).expand(B, W).contiguous()
+    pool.fill(g, table[:1], [L])
+    q = base.rows(g, H, B * n, D, torch.bfloat16)
+    cu, lens = base.prefix([n] * B), base.i32([L - b for b in range(B)])
+    # (not bit for bit: where keys are cut depends on all sequences' lengths)
+    o, bound = base.R.attention(q, lambda b, h: pool.rows(0, table[b], L - b, h // 2), lambda b, h: pool.rows(1, table[b], L - b, h // 2), cu, [L - b for b in range(B)], 1, q.dtype)
+    for at in sorted({1, 2, B // 2, B - 1}):
+        off = list(cu)
+        off[at] = wrong
+        if off[at] <= off[at + 1] <= B * n and off[at + 1] - off[at] <= n:      # (the entry makes a sequence of its own, over others' rows)
+            continue
+        out = torch.full_like(q, 2.0)
+        fastar.kv8_attention(q, *pool.args(), table, lens, base.i32(off), n, L, out=out)
+        assert fastar.dense_last_status() == fastar.ERR_BOUNDS
+        for b in range(B):
+            rows = slice(n * b, n * b + n)
+            if b in (at - 1, at):
+                assert bool((out[:, rows] == 2.0).all()), (at, b)
+            else:
+                assert bool(((out[:, rows].double() - o[:, rows]).abs() <= bound[:, rows]).all()), (at, b)
