@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(kFewThreads, FewConf<D, NR>::CTAS) few_kernel(
           v.z = fmaf(x4.z, f[w], v.z);
           v.w = fmaf(x4.w, f[w], v.w);
         }
-        if (whole) *reinterpret_cast<uint2*>(out + col) = make_uint2(narrow2<T>(v.x * inv, v.y * inv), narrow2<T>(v.z * inv, v.w * inv));
+        if (whole) *reinterpret_cast<uint2*>(out + col) = make_uint2(narrow2<T>(times(v.x, inv), times(v.y, inv)), narrow2<T>(times(v.z, inv), times(v.w, inv)));
         else if (SMALL) *reinterpret_cast<float4*>(join + r * SM::pitch + col) = v;        // (this thread has read what was there)
         else *reinterpret_cast<float4*>(a.few_o + static_cast<int64_t>(place + r) * D + col) = v;
       }

@@ -109,11 +109,13 @@ __device__ __forceinline__ void dense_row(const DenseArgs& a, int b, int t, int 
   }
 }
 
-// The row's end: into `out`, or as a part of it.
+// The row's end: into `out`, or as a part of it.  inv = 0: only logits of -inf were seen, the row is zeros whatever o holds (0 x NaN).
+__device__ __forceinline__ float times(float o, float inv) { return inv == 0.f ? 0.f : o * inv; }
 template <class T, int D>
 __device__ __forceinline__ void store_cols(T* row, int lane, const float (&o)[D / 32], float inv) {
-  if constexpr (D == 128) *reinterpret_cast<uint2*>(row + lane * 4) = make_uint2(narrow2<T>(o[0] * inv, o[1] * inv), narrow2<T>(o[2] * inv, o[3] * inv));
-  else *reinterpret_cast<uint32_t*>(row + lane * 2) = narrow2<T>(o[0] * inv, o[1] * inv);
+  if constexpr (D == 128)
+    *reinterpret_cast<uint2*>(row + lane * 4) = make_uint2(narrow2<T>(times(o[0], inv), times(o[1], inv)), narrow2<T>(times(o[2], inv), times(o[3], inv)));
+  else *reinterpret_cast<uint32_t*>(row + lane * 2) = narrow2<T>(times(o[0], inv), times(o[1], inv));
 }
 // (`whole`: all that the row sees is in [k0, k1), and it goes into `out`; otherwise a part of it, to part_o and part_ml.)
 template <class T, int D, bool PAGED>

@@ -333,3 +333,27 @@ def test_wrong_prefix_sums_reach_their_own_sequences_only(fastar, B, n, L, wrong
                 assert bool((out[:, rows] == 2.0).all()), (at, b)
             else:
                 assert bool(((out[:, rows].double() - o[:, rows]).abs() <= bound[:, rows]).all()), (at, b)
+
+
+@pytest.mark.parametrize("past", [0, 20, 6000])
+@pytest.mark.parametrize("n", [1, 5, 140])
+def test_rows_of_minus_infinity_take_no_values(fastar, n, past):  # noqa: F811
+    """A row that sees only logits of -inf gives zeros, also where the values that it sees are no numbers."""
+    g, D, PT, KV, H = base.gen(91), 128, 64, 1, 2
+    L = past + n
+    W = -(-L // PT)
+    pool, table = base.Pool(W, KV, PT, D), torch.arange(W, dtype=torch.int32, device=base.DEV).view(1, W)
+    pool.fill(g, table, [L])
+    pool.codes[0][..., 0] = 0x38                                               # 1
+    pool.codes[1][..., 3] = 0x7F
+    q = base.rows(g, H, n, D, torch.bfloat16)
+    q[0, :, 0] = -float("inf")
+    out = fastar.kv8_attention(q, *pool.args(), table, base.i32([L]), base.i32([0, n]), n, L)
+    assert bool((out[0] == 0).all()) and bool(torch.isnan(out[1, :, 3]).all()) and bool(torch.isfinite(out[1, :, 4:]).all())
+    k, v = base.rows(g, KV, L, D, torch.bfloat16), base.rows(g, KV, L, D, torch.bfloat16)
+    k[..., 0], v[..., 3] = 1.0, float("nan")
+    q = base.rows(g, H, L, D, torch.bfloat16)
+    q[0, :, 0] = -float("inf")
+    for frame in (0, 1, 7):
+        out = fastar.packed_attention(q, k, v, base.i32([0, L]), L, frame_len=frame)
+        assert bool((out[0] == 0).all()) and bool(torch.isnan(out[1, :, 3]).all()) and bool(torch.isfinite(out[1, :, 4:]).all())
